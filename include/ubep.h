@@ -412,6 +412,123 @@ int ubep_wait_arrivals(ubep_buffer_t *buf, void *cuda_stream);
 int ubep_combine_sharded(ubep_buffer_t *buf, const void *const *y_peers /*[dev]*/, const float *topk_w /*[dev]*/,
                          int32_t T, void *out_local /*[dev]*/, void *cuda_stream);
 
+/* ----------------------------------------------------------------------------------------
+ * The rest of a mixture-of-experts layer: the router in front of ubep_dispatch, the experts'
+ * products between it and ubep_combine, and the gradients of both.
+ *
+ * A layer:   ubep_route(logits) -> topk_idx, topk_w
+ *            ubep_dispatch(x, topk_idx, topk_w)
+ *            ubep_expert_gated(rows as received) -> h,  ubep_expert_linear(h) -> y
+ *            ubep_combine(y, topk_w) -> out
+ * In training the weight of a row is taken in the epilogue of ubep_expert_linear
+ * (row_scale = UBEP_VIEW_RECV_WEIGHT) and ubep_combine is given weights of one.  Its gradient
+ * is then ubep_dispatch of the output's gradient with the same table (on a second buffer), the
+ * experts' backward calls, and ubep_combine of the rows' gradients with weights of one; the gradient
+ * of topk_w[t][j] is the row weight's gradient at slot_row[t][j].
+ *
+ * All of them are asynchronous on `cuda_stream`, keep nothing between calls and need no state
+ * of their own, so calls on different streams may overlap as long as their outputs are
+ * different memory.  Sums, weights and activations are taken in 32 bits; every bf16 result is
+ * rounded once from them.  No atomics: results do not depend on timing.  Outputs may not overlap
+ * inputs or each other except where a call says so.
+ */
+enum { UBEP_LOGITS_F32 = 0, UBEP_LOGITS_BF16 = 1 };
+
+/*
+ * Router: slot j of token t gets the expert with the j-th largest logit (ties: the lower id
+ * first) and its weight, softmax over the chosen experts (renormalize != 0) or its probability
+ * among all experts (renormalize = 0).  Logits of minus infinity and NaN mark an expert that the
+ * token may not choose; where fewer than k are left the last slots get id -1 and weight 0.
+ * (A logit of plus infinity makes the token's weights NaN, as the formula has it.)
+ * logits [dev] [T, E] of `logits_type`; topk_idx [dev] int32 [T, k], topk_w [dev] fp32 [T, k]:
+ * what ubep_dispatch takes.  E in [1, 65535], k in [1, 32].  One launch.
+ */
+int ubep_route(const void *logits /*[dev]*/, int logits_type, int32_t T, int32_t E, int32_t k, int32_t renormalize,
+               int32_t *topk_idx /*[dev]*/, float *topk_w /*[dev]*/, int32_t device, void *cuda_stream);
+
+/*
+ * Gradient of the weights with respect to the logits, of all E experts: grad_w [dev] fp32
+ * [T, k] in, grad_logits [dev] [T, E] of `logits_type` out (it may not be the logits).  topk_idx as
+ * ubep_route left it; slots that hold no expert's id, or the id of an earlier slot, count as empty.
+ * One launch.
+ */
+int ubep_route_backward(const void *logits /*[dev]*/, int logits_type, const int32_t *topk_idx /*[dev]*/,
+                        const float *grad_w /*[dev]*/, int32_t T, int32_t E, int32_t k, int32_t renormalize,
+                        void *grad_logits /*[dev]*/, int32_t device, void *cuda_stream);
+
+/*
+ * Which rows belong to which expert.  Arrays of rows are laid out like receive regions,
+ * [num_ranks, rows_per_rank_cap, width]; expert e of rank r = e / (num_experts / num_ranks) has rows
+ * offset[e] .. offset[e] + count[e] - 1 of region r (what passes the region's end is left out,
+ * as in dispatch).  Rows of no segment are neither read nor written; segments may not overlap.
+ */
+typedef struct {
+    const int32_t *offset;     /* [dev] [num_experts]                                          */
+    const int32_t *count;      /* [dev] [num_experts]                                          */
+    int32_t num_experts;       /* a multiple of num_ranks                                      */
+    int32_t num_ranks;
+    int32_t rows_per_rank_cap;
+    int32_t device;            /* CUDA device ordinal                                          */
+    int32_t *status;           /* [dev] word for UBEP_ERR_TIMEOUT, or NULL                     */
+} ubep_expert_rows_t;
+
+/*
+ * The segments that the last dispatch on this buffer left (and its status word, which
+ * ubep_status reads).  Needs one row per (token, slot): UBEP_ERR_ARG with dedup = 1, whose rows are not
+ * in expert order.  In sharded use (ubep_set_peers) these are this rank's experts and its
+ * region alone: num_ranks = 1, arrays [1, cap, width].  Nothing is launched.
+ */
+int ubep_expert_rows(ubep_buffer_t *buf, ubep_expert_rows_t *rows /*[host]*/);
+
+enum { UBEP_ACT_NONE = 0, UBEP_ACT_SILU = 1, UBEP_ACT_GELU = 2 /* x Phi(x) */, UBEP_ACT_RELU = 3 };
+
+/*
+ * Gated feed-forward block: h = act(x Wg_e^T) * (x Wu_e^T) for every row x of expert e.
+ * x [dev]: bf16 [R, cap, H]; with x_scale [dev] fp32 [R, cap, H / 128], e4m3 [R, cap, H] with one
+ * scale per 128 channels as an FP8 dispatch delivers them (H a multiple of 128), and scratch [dev]
+ * bf16 [R, cap, H] for the rows as bf16.  w [dev] bf16 [E, 2, I, H]: the gate's matrix, then the other.
+ * h [dev] bf16 [R, cap, I].  pre [dev] bf16 [R, cap, 2, I] or NULL: both products, for
+ * ubep_expert_gated_backward.  H and I multiples of 8.  One launch, two with FP8 rows.
+ */
+int ubep_expert_gated(const ubep_expert_rows_t *rows /*[host]*/, const void *x /*[dev]*/, const float *x_scale /*[dev]*/,
+                      const void *w /*[dev]*/, int32_t H, int32_t I, int act, void *h /*[dev]*/, void *pre /*[dev]*/,
+                      void *scratch /*[dev]*/, void *cuda_stream);
+
+/*
+ * Its gradients: with dg = grad_h u act'(g) and du = grad_h act(g), g and u from pre,
+ * grad_x = dg Wg + du Wu ([dev] bf16 [R, cap, H]) and grad_w = [dg^T x, du^T x] ([dev] bf16 [E, 2, I, H]; zero for an
+ * expert without rows).  Either may be NULL.  grad_pre [dev] bf16 [R, cap, 2, I]: room for dg and du,
+ * rounded to bf16 for the products; may be pre itself.  x, x_scale, scratch as above (scratch is needed for grad_w
+ * alone).  Up to four launches.
+ */
+int ubep_expert_gated_backward(const ubep_expert_rows_t *rows /*[host]*/, const void *x /*[dev]*/,
+                               const float *x_scale /*[dev]*/, const void *w /*[dev]*/, const void *pre /*[dev]*/,
+                               const void *grad_h /*[dev]*/, int32_t H, int32_t I, int act, void *grad_pre /*[dev]*/,
+                               void *grad_x /*[dev]*/, void *grad_w /*[dev]*/, void *scratch /*[dev]*/, void *cuda_stream);
+
+/*
+ * Product with its epilogue: y = row_scale * act(x W_e^T + bias_e) + residual for every row x of expert e.
+ * x [dev] bf16 [R, cap, K]; w [dev] bf16 [E, N, K]; bias [dev] bf16 [E, N], row_scale [dev] fp32 [R, cap], residual [dev]
+ * bf16 [R, cap, N] (may be y itself), each or NULL.  y [dev] bf16 [R, cap, N].  pre [dev] bf16 [R, cap, N] or NULL:
+ * x W_e^T + bias_e, for the backward call.  K and N multiples of 8.  One launch.
+ */
+int ubep_expert_linear(const ubep_expert_rows_t *rows /*[host]*/, const void *x /*[dev]*/, const void *w /*[dev]*/,
+                       const void *bias /*[dev]*/, const float *row_scale /*[dev]*/, const void *residual /*[dev]*/,
+                       int32_t K, int32_t N, int act, void *y /*[dev]*/, void *pre /*[dev]*/, void *cuda_stream);
+
+/*
+ * Its gradients, with dz = row_scale grad_y act'(pre): grad_x = dz W ([dev] bf16 [R, cap, K]), grad_w = dz^T x ([dev] bf16
+ * [E, N, K]), grad_bias = column sums of dz ([dev] bf16 [E, N]), grad_row_scale = <grad_y, act(pre)> ([dev] fp32 [R, cap]; needs
+ * row_scale); each may be NULL, and experts without rows get zeros.  (The residual's gradient is grad_y.)  pre and
+ * grad_pre ([dev] bf16 [R, cap, N], room for dz rounded to bf16; may be pre itself unless grad_bias is
+ * asked for) are needed with an activation or row_scale and not read without.  Up to four launches.
+ */
+int ubep_expert_linear_backward(const ubep_expert_rows_t *rows /*[host]*/, const void *x /*[dev]*/, const void *w /*[dev]*/,
+                                const void *pre /*[dev]*/, const float *row_scale /*[dev]*/, const void *grad_y /*[dev]*/,
+                                int32_t K, int32_t N, int act, void *grad_pre /*[dev]*/, void *grad_x /*[dev]*/,
+                                void *grad_w /*[dev]*/, void *grad_bias /*[dev]*/, float *grad_row_scale /*[dev]*/,
+                                void *cuda_stream);
+
 /* Device address and shape (unused dims = 1) of one arena array; valid until destroy. */
 int ubep_view(ubep_buffer_t *buf, int which, void **dev_ptr /*[host]*/, int64_t shape[4] /*[host]*/);
 

@@ -49,13 +49,24 @@ EXPORTS = ["ubep_buffer_bytes", "ubep_buffer_create", "ubep_buffer_destroy", "ub
            "ubep_last_cuda_error", "ubep_strerror", "ubep_map_workers",
            "ubep_sync_wire_bytes", "ubep_sync_attach", "ubep_dispatch_sync", "ubep_sync_view",
            "ubep_sync_scan_sentinel",
-           "ubep_set_peers", "ubep_dispatch_sharded", "ubep_wait_arrivals", "ubep_combine_sharded"]
+           "ubep_set_peers", "ubep_dispatch_sharded", "ubep_wait_arrivals", "ubep_combine_sharded",
+           "ubep_route", "ubep_route_backward", "ubep_expert_rows", "ubep_expert_gated", "ubep_expert_gated_backward",
+           "ubep_expert_linear", "ubep_expert_linear_backward"]
+UBEP_LOGITS_F32, UBEP_LOGITS_BF16 = 0, 1
+UBEP_ACT_NONE, UBEP_ACT_SILU, UBEP_ACT_GELU, UBEP_ACT_RELU = 0, 1, 2, 3
+ACT_NAMES = {"none": 0, "silu": 1, "gelu": 2, "relu": 3}
 
 
 class ubep_config_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("num_ranks", "num_experts", "hidden", "topk", "max_tokens", "rows_per_rank_cap",
                  "num_src_ranks", "payload", "dedup", "device", "pipeline", "num_ctas")]
+
+
+class ubep_expert_rows_t(ctypes.Structure):
+    _fields_ = [("offset", ctypes.c_void_p), ("count", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("num_experts", "num_ranks", "rows_per_rank_cap", "device")] + \
+               [("status", ctypes.c_void_p)]
 
 
 _lib = None
@@ -117,9 +128,25 @@ def load() -> ctypes.CDLL:
     lib.ubep_wait_arrivals.restype, lib.ubep_wait_arrivals.argtypes = ctypes.c_int, [vp, vp]
     lib.ubep_combine_sharded.restype = ctypes.c_int
     lib.ubep_combine_sharded.argtypes = [vp, vp, vp, i32, vp, vp]
+    lib.ubep_route.restype = ctypes.c_int
+    lib.ubep_route.argtypes = [vp, ctypes.c_int, i32, i32, i32, i32, vp, vp, i32, vp]
+    lib.ubep_route_backward.restype = ctypes.c_int
+    lib.ubep_route_backward.argtypes = [vp, ctypes.c_int, vp, vp, i32, i32, i32, i32, vp, i32, vp]
+    rowsp = ctypes.POINTER(ubep_expert_rows_t)
+    lib.ubep_expert_rows.restype, lib.ubep_expert_rows.argtypes = ctypes.c_int, [vp, rowsp]
+    lib.ubep_expert_gated.restype = ctypes.c_int
+    lib.ubep_expert_gated.argtypes = [rowsp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp, vp]
+    lib.ubep_expert_gated_backward.restype = ctypes.c_int
+    lib.ubep_expert_gated_backward.argtypes = [rowsp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp, vp, vp]
+    lib.ubep_expert_linear.restype = ctypes.c_int
+    lib.ubep_expert_linear.argtypes = [rowsp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp]
+    lib.ubep_expert_linear_backward.restype = ctypes.c_int
+    lib.ubep_expert_linear_backward.argtypes = [rowsp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp, vp, vp, vp]
     native = _load_native()
     native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
-                  (lib.ubep_dispatch, lib.ubep_combine, lib.ubep_get_dispatch_layout, lib.ubep_dispatch_sync)))
+                  (lib.ubep_dispatch, lib.ubep_combine, lib.ubep_get_dispatch_layout, lib.ubep_dispatch_sync,
+                   lib.ubep_route, lib.ubep_route_backward, lib.ubep_expert_gated, lib.ubep_expert_gated_backward,
+                   lib.ubep_expert_linear, lib.ubep_expert_linear_backward)))
     _lib = lib
     return lib
 
@@ -374,6 +401,89 @@ def ubep_combine_sharded(buf, y_peers: torch.Tensor, topk_w: torch.Tensor, T: in
            "ubep_combine_sharded", buf)
 
 
+def ubep_expert_rows(buf) -> ubep_expert_rows_t:
+    rows = ubep_expert_rows_t()
+    _check(load().ubep_expert_rows(buf, ctypes.byref(rows)), "ubep_expert_rows", buf)
+    return rows
+
+
+# ------------------------------------------------------------------ router and experts
+#
+# Sizes are taken from the tensors; a tensor of another type, shape or device raises ValueError.  Outputs left at None
+# are allocated (rows of no segment are not written).  The arithmetic is described in include/ubep.h.
+
+class ExpertRows:
+    """Which rows of arrays [ranks, rows, width] belong to which expert: ``offset`` and ``count``, int32 [experts] on the
+    GPU, relative to the expert's rank's region; ``status``, int32 [1], gets UBEP_ERR_TIMEOUT (None: nobody is told)."""
+    __slots__ = ("offset", "count", "status")
+
+    def __init__(self, offset: torch.Tensor, count: torch.Tensor, status: Optional[torch.Tensor] = None):
+        self.offset, self.count, self.status = offset, count, status
+
+
+def _done(out, where):
+    if type(out) is int:
+        _check(out, where)
+    return out
+
+
+def _act(name) -> int:
+    code = ACT_NAMES.get(name)
+    if code is None:
+        raise ValueError(f"act: {name!r} is none of {', '.join(ACT_NAMES)}")
+    return code
+
+
+def route(logits: torch.Tensor, topk: int, renormalize: bool = True, topk_idx=None, topk_w=None, stream=None):
+    """The ``topk`` largest logits of every token and their softmax weights: (topk_idx int32, topk_w fp32), [tokens, topk]."""
+    load()
+    return _done(_native.route(logits, topk, renormalize, topk_idx, topk_w, stream), "ubep_route")
+
+
+def route_backward(logits: torch.Tensor, topk_idx: torch.Tensor, grad_w: torch.Tensor, renormalize: bool = True,
+                   grad_logits=None, stream=None) -> torch.Tensor:
+    """Gradient of ``route``'s weights with respect to the logits."""
+    load()
+    return _done(_native.route_backward(logits, topk_idx, grad_w, renormalize, grad_logits, stream), "ubep_route_backward")
+
+
+def expert_gated(rows: ExpertRows, x: torch.Tensor, w: torch.Tensor, act: str = "silu", x_scale=None, out=None, pre=None,
+                 stream=None) -> torch.Tensor:
+    """act(x Wg^T) * (x Wu^T): x [ranks, rows, H] (bf16; e4m3 with ``x_scale`` [ranks, rows, H / 128]; or the bytes of a receive
+    region), w [experts, 2, I, H] -> [ranks, rows, I].  ``pre`` [ranks, rows, 2, I] gets both products, for the backward call."""
+    load()
+    return _done(_native.expert_gated(rows.offset, rows.count, rows.status, x, x_scale, w, _act(act), out, pre, stream),
+                 "ubep_expert_gated")
+
+
+def expert_gated_backward(rows: ExpertRows, x: torch.Tensor, w: torch.Tensor, pre: torch.Tensor, grad_h: torch.Tensor,
+                          act: str = "silu", x_scale=None, grad_x=None, grad_w=None, grad_pre=None, stream=None):
+    """(grad_x, grad_w) of ``expert_gated``.  False in the place of one of them: not computed.  ``grad_pre``: room for the gradients
+    of ``pre``, which may be ``pre`` itself (None: allocated for the call)."""
+    load()
+    return _done(_native.expert_gated_backward(rows.offset, rows.count, rows.status, x, x_scale, w, pre, grad_h, _act(act), grad_pre,
+                                               grad_x, grad_w, stream), "ubep_expert_gated_backward")
+
+
+def expert_linear(rows: ExpertRows, x: torch.Tensor, w: torch.Tensor, bias=None, row_scale=None, residual=None, act: str = "none",
+                  out=None, pre=None, stream=None) -> torch.Tensor:
+    """row_scale * act(x W^T + bias) + residual: x [ranks, rows, K], w [experts, N, K], bias [experts, N], row_scale [ranks, rows]
+    fp32, residual [ranks, rows, N] -> [ranks, rows, N].  ``pre`` gets x W^T + bias, for the backward call."""
+    load()
+    return _done(_native.expert_linear(rows.offset, rows.count, rows.status, x, w, bias, row_scale, residual, _act(act), out, pre,
+                                       stream), "ubep_expert_linear")
+
+
+def expert_linear_backward(rows: ExpertRows, x: torch.Tensor, w: torch.Tensor, grad_y: torch.Tensor, pre=None, row_scale=None,
+                           act: str = "none", grad_x=None, grad_w=None, grad_bias=None, grad_row_scale=None, grad_pre=None,
+                           stream=None):
+    """(grad_x, grad_w, grad_bias, grad_row_scale) of ``expert_linear``.  grad_x and grad_w are allocated where they are None and
+    left out where they are False; grad_bias and grad_row_scale are computed into a tensor, or a new one for True."""
+    load()
+    return _done(_native.expert_linear_backward(rows.offset, rows.count, rows.status, x, w, grad_y, pre, row_scale, _act(act), grad_pre,
+                                                grad_x, grad_w, grad_bias, grad_row_scale, stream), "ubep_expert_linear_backward")
+
+
 # ------------------------------------------------------------------------ convenience
 
 class Buffer:
@@ -451,6 +561,16 @@ class Buffer:
         if rc:
             _check(rc, "ubep_combine", self.handle)
         return out
+
+    def expert_rows(self) -> ExpertRows:
+        """The segments the last dispatch left, for the experts' calls (one row per (token, slot): not with dedup).  After
+        ``ubep_set_peers`` they are those of this rank alone, on arrays [1, cap, width]."""
+        r = ubep_expert_rows(self.handle)
+        base = self.arena.data_ptr()
+
+        def words(ptr, n):
+            return self.arena[ptr - base: ptr - base + 4 * n].view(torch.int32)
+        return ExpertRows(words(r.offset, r.num_experts), words(r.count, r.num_experts), words(r.status, 1))
 
     def status(self) -> int:
         return ubep_status(self.handle)

@@ -1,0 +1,779 @@
+// The experts' products on ragged segments of rows: the gated feed-forward block, the product with bias, activation, row
+// weight and residual, and both backward passes.
+//
+//   forward   D^T[feature, row] = W[feature, :] . x[row, :]              W and x along the contraction
+//   rows' gradient   D^T[feature, row] = sum_n W[n, feature] dz[row, n]  W across it
+//   weights' gradient   D[n, feature] = sum_row dz[row, n] x[row, feature]   both across it, the rows being the contraction
+//
+// One persistent kernel, one CTA per SM: a warp loads operand tiles with tensor-map copies into a ring in shared memory, a warp
+// issues tcgen05.mma, eight warps turn sums in tensor memory into results.  The rows are the N dimension of the
+// instruction (a multiple of 16), the features its M (128 per CTA): a segment of 139 rows costs 144, where rows as M would
+// cost 256, and sixteen rows of a decode step cost sixteen.  Each tile of rows is multiplied with two tiles of features (gate and
+// up of the same features, or 256 features of one matrix), which halves the shared-memory and L2 traffic per
+// multiplication: a step of 64 of the contraction brings 64 KB for 1024 cycles of the tensor cores.
+#include <cstdint>
+#include <atomic>
+
+#include "../../include/ubep.h"
+#include "ubep_experts.cuh"
+#include "ubep_launch.cuh"
+#include "ubep_tensor.cuh"
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "ubep_experts.h"
+
+namespace ubep {
+
+namespace {
+
+enum { kGated = 0, kLinear = 1, kRowsGrad = 2, kWeightsGrad = 3 };
+
+constexpr int kGemmThreads = 320;        // a loading warp, a multiplying warp, eight warps for the results
+constexpr int kResultWarps = 8;
+constexpr int kStepK = 64;               // of the contraction per stage: 128 bytes of bf16, the swizzle's width
+constexpr int kHalfBytes = 128 * 128;    // 128 features of one stage
+constexpr int kMaxRing = 8;
+constexpr int kStagePitch = 36;          // floats per row of a warp's transposition tile: conflict-free both ways
+constexpr int kStageFloats = 16 * kStagePitch;
+constexpr int kColumns = 512;            // tensor memory: all of it (one CTA per SM)
+
+struct Product {
+    Segments seg;
+    int F;           // features (of the gated block: inner features)
+    int K;           // contraction (weights' gradient: the segment's rows instead)
+    int FB;          // weights' gradient: features of x
+    int most;        // rows per tile at most; columns of one accumulator
+    int stages, stage_bytes, accs;
+    int act;
+    uint16_t *out, *pre;
+    const uint16_t *bias, *residual;
+    const float* row_scale;
+    int32_t* status;
+};
+
+struct Shared {
+    uint64_t full[kMaxRing], empty[kMaxRing], acc_full[2], acc_empty[2], drained;
+    uint32_t tmem;
+    int abort;
+};
+
+// Waits of a whole warp; all lanes agree on the outcome.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity, Shared* sh, int32_t* status) {
+    const bool ok = mbar_wait_idle(bar, parity, &sh->abort);
+    if (__all_sync(0xffffffffu, ok)) return true;
+    if ((threadIdx.x & 31) == 0) {
+        *(volatile int*)&sh->abort = 1;
+        if (status) report(status, kErrTimeout);
+    }
+    return false;
+}
+
+// Place of a tile: expert, rows and features.
+struct Tile {
+    int e, row, rows, f0, fb0;   // global row of its first row, its rows, first feature, weights' gradient: first feature of x
+};
+
+template <int MODE, int CG>
+struct Walk {
+    TileWalk w;
+    const Product& p;
+    int per_row_tile, fb_tiles;
+    static constexpr int kFeatures = (MODE == kGated ? 128 : 256) * CG;
+    static constexpr bool kEvery = MODE == kWeightsGrad;
+    static constexpr int kUnit = 16 * CG;
+    __device__ __forceinline__ explicit Walk(const Product& p_) : p(p_) {
+        fb_tiles = kEvery ? (p.FB + 255) / 256 : 1;
+        per_row_tile = (p.F + kFeatures - 1) / kFeatures * fb_tiles;
+        w.base = w.before = 0;
+        w.load(p.seg, per_row_tile, p.most, kEvery);
+    }
+    __device__ __forceinline__ bool find(int t, Tile& o) {
+        int first, rows, place;
+        if (!w.find(p.seg, per_row_tile, p.most, kEvery, t, o.e, first, rows, place)) return false;
+        if (kEvery) {
+            // (neighbours share the tile of the first operand)
+            o.f0 = place / fb_tiles * kFeatures;
+            o.fb0 = place % fb_tiles * 256;
+            o.row = first;
+            o.rows = rows;
+        } else {
+            // (neighbours share the tile of the weights, which comes from memory once)
+            const int n = row_tiles(rows, p.most);
+            const int piece = ((rows + n - 1) / n + kUnit - 1) / kUnit * kUnit;
+            const int i = place % n;
+            o.f0 = place / n * kFeatures;
+            o.fb0 = 0;
+            o.row = first + i * piece;
+            o.rows = min(piece, rows - i * piece);
+        }
+        return true;
+    }
+};
+
+__device__ __forceinline__ uint4 ld_vec(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
+
+template <int MODE, int CG>
+__global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
+                                                                const __grid_constant__ CUtensorMap map_b, const Product p) {
+    extern __shared__ uint8_t dynamic[];
+    __shared__ Shared sh;
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
+    float* stage_tiles = reinterpret_cast<float*>(ring + (size_t)p.stages * p.stage_bytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < p.stages; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.acc_full[i], 1);
+            mbar_init(&sh.acc_empty[i], kResultWarps);
+        }
+        mbar_init(&sh.drained, 1);
+        sh.abort = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        if (lane == 0) {
+            map_prefetch(&map_a);
+            map_prefetch(&map_b);
+        }
+        tmem_alloc<CG>(&sh.tmem, kColumns);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t*)&sh.tmem;
+    griddep_wait();
+    const int unit = blockIdx.x, units = gridDim.x;
+    Walk<MODE, CG> walk(p);
+    Tile t;
+    constexpr bool kAcross = MODE == kRowsGrad || MODE == kWeightsGrad;   // the features' operand
+    constexpr int kBoxRows = 32;
+    if (warp == 0) {
+        // ------------------------------------------------------------------ loads
+        int s = 0, used = 0;
+        unsigned phase = 0;
+        bool ok = true;
+        for (int id = unit; ok && walk.find(id, t); id += units) {
+            const int K = MODE == kWeightsGrad ? t.rows : p.K;
+            const int steps = (K + kStepK - 1) / kStepK;
+            const bool two = MODE == kGated || t.f0 + 128 < p.F;
+            const int boxes = MODE == kWeightsGrad ? 4 : (t.rows + kBoxRows - 1) / kBoxRows;
+            const unsigned bytes = (two ? 2 : 1) * kHalfBytes + boxes * (MODE == kWeightsGrad ? 8192 : kBoxRows * 128);
+            for (int k = 0; k < steps; ++k) {
+                ok = warp_wait(&sh.empty[s], phase ^ 1, &sh, p.status);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t a = smem_u32(ring + (size_t)s * p.stage_bytes), b = a + 2 * kHalfBytes, bar = smem_u32(&sh.full[s]);
+                    mbar_arrive_expect_tx(&sh.full[s], bytes);
+                    const int k0 = k * kStepK;
+                    if constexpr (MODE == kGated) {
+                        tile_load<CG>(a, &map_a, k0, t.f0, 2 * t.e, bar);
+                        tile_load<CG>(a + kHalfBytes, &map_a, k0, t.f0, 2 * t.e + 1, bar);
+                    } else if constexpr (MODE == kLinear) {
+                        tile_load<CG>(a, &map_a, k0, t.f0, t.e, bar);
+                        if (two) tile_load<CG>(a + kHalfBytes, &map_a, k0, t.f0 + 128, t.e, bar);
+                    } else {
+                        const int y = MODE == kRowsGrad ? k0 : t.row + k0, z = MODE == kRowsGrad ? t.e : 0;
+                        for (int j = 0; j < (two ? 4 : 2); ++j) tile_load<CG>(a + j * 8192, &map_a, t.f0 + 64 * j, y, z, bar);
+                    }
+                    if constexpr (MODE == kWeightsGrad)
+                        for (int j = 0; j < 4; ++j) tile_load<CG>(b + j * 8192, &map_b, t.fb0 + 64 * j, t.row + k0, 0, bar);
+                    else
+                        for (int j = 0; j < boxes; ++j) tile_load<CG>(b + j * kBoxRows * 128, &map_b, k0, t.row + j * kBoxRows, 0, bar);
+                }
+                __syncwarp();
+                ++used;
+                if (++s == p.stages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+        if (!ok) {
+            // nothing may still be on its way into this CTA's shared memory when it leaves: the last copy of every stage
+            for (int i = 0; i < p.stages && i < used; ++i) {
+                s = s ? s - 1 : p.stages - 1;
+                if (s == p.stages - 1) phase ^= 1;
+                mbar_wait(&sh.full[s], phase, nullptr);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ products
+        int s = 0, acc = 0;
+        unsigned phase = 0, acc_phase = 0;
+        bool ok = true;
+        for (int id = unit; ok && walk.find(id, t); id += units) {
+            const int K = MODE == kWeightsGrad ? t.rows : p.K;
+            const int steps = (K + kStepK - 1) / kStepK;
+            if (steps == 0) continue;
+            const bool two = MODE == kGated || t.f0 + 128 < p.F;
+            const int n = MODE == kWeightsGrad ? 256 : (t.rows + 15) / 16 * 16;
+            const uint32_t idesc = instruction(128, n, kAcross, MODE == kWeightsGrad);
+            const uint32_t d = tmem + acc * 2 * p.most;
+            ok = warp_wait(&sh.acc_empty[acc], acc_phase ^ 1, &sh, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            for (int k = 0; k < steps; ++k) {
+                ok = warp_wait(&sh.full[s], phase, &sh, p.status);
+                if (!ok) break;
+                uint8_t* stage = ring + (size_t)s * p.stage_bytes;
+                const int left = K - k * kStepK;
+                if constexpr (MODE == kWeightsGrad) {
+                    if (left < kStepK) {
+                        // rows behind the segment are another expert's, or nobody's: whatever they hold must not be multiplied
+                        const int end = (left + 15) / 16 * 16;
+                        for (int r = left; r < end; ++r)
+                            for (int v = lane; v < 64; v += 32)
+                                *reinterpret_cast<uint4*>(stage + (v >> 3) * 8192 + r * 128 + (v & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                }
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t a = smem_u32(stage), b = a + 2 * kHalfBytes;
+                    const int parts = left < kStepK ? (left + 15) / 16 : 4;
+                    for (int j = 0; j < parts; ++j) {
+                        const uint64_t da = kAcross ? operand(a + j * 2048, 8192, 1024) : operand(a + j * 32, 16, 1024);
+                        const uint64_t db = MODE == kWeightsGrad ? operand(b + j * 2048, 8192, 1024) : operand(b + j * 32, 16, 1024);
+                        mma_f16<CG>(d, da, db, idesc, (k | j) != 0);
+                        if (two) mma_f16<CG>(d + p.most, da + (kHalfBytes >> 4), db, idesc, (k | j) != 0);
+                    }
+                    mma_commit<CG>(&sh.empty[s]);
+                    if (k == steps - 1) mma_commit<CG>(&sh.acc_full[acc]);
+                }
+                __syncwarp();
+                if (++s == p.stages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
+            if (++acc == p.accs) {
+                acc = 0;
+                acc_phase ^= 1;
+            }
+        }
+        if (!ok) {   // no product may still be running when the tensor memory is given back
+            if (elect_one()) mma_commit<CG>(&sh.drained);
+            __syncwarp();
+            mbar_wait(&sh.drained, 0, nullptr);
+        }
+    } else {
+        // ------------------------------------------------------------------ results
+        const int quarter = warp & 3, group = (warp - 2) >> 2;   // lanes of tensor memory this warp may read; which columns
+        float* tile = stage_tiles + (warp - 2) * kStageFloats;
+        int acc = 0;
+        unsigned acc_phase = 0;
+        bool ok = true;
+        for (int id = unit; ok && walk.find(id, t); id += units) {
+            const bool empty = MODE == kWeightsGrad && t.rows == 0;
+            if (!empty) {
+                ok = warp_wait(&sh.acc_full[acc], acc_phase, &sh, p.status);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * 2 * p.most;
+            if constexpr (MODE == kGated) {
+                const int f = t.f0 + quarter * 32 + (lane & 3) * 8;
+                for (int c = group * 8; c < t.rows; c += 16) {
+                    float g[8], u[8];
+                    tmem_ld8x2(d + c, d + p.most + c, g, u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        tile[i * kStagePitch + lane] = g[i];
+                        tile[(8 + i) * kStagePitch + lane] = u[i];
+                    }
+                    __syncwarp();
+                    const float* at = tile + (lane >> 2) * kStagePitch + (lane & 3) * 8;
+#pragma unroll
+                    for (int i = 0; i < 8; i += 4) {
+                        *reinterpret_cast<float4*>(g + i) = *reinterpret_cast<const float4*>(at + i);
+                        *reinterpret_cast<float4*>(u + i) = *reinterpret_cast<const float4*>(at + 8 * kStagePitch + i);
+                    }
+                    __syncwarp();
+                    const int r = c + (lane >> 2);
+                    if (r < t.rows && f < p.F) {
+                        const int64_t row = t.row + r;
+                        if (p.pre) {
+                            st_vec(p.pre + row * 2 * p.F + f, pack8(g));
+                            st_vec(p.pre + (row * 2 + 1) * p.F + f, pack8(u));
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) g[i] = act_value(g[i], p.act) * u[i];
+                        st_vec(p.out + row * p.F + f, pack8(g));
+                    }
+                }
+            } else if constexpr (MODE == kWeightsGrad) {
+                for (int h = 0; h < 2; ++h) {
+                    const int f = t.f0 + h * 128 + quarter * 32 + lane;
+                    if (f - lane >= p.F) break;
+                    uint16_t* out = p.out + ((int64_t)t.e * p.F + f) * p.FB + t.fb0;
+                    const int cols = min(256, p.FB - t.fb0);
+                    for (int c = group * 16; c < cols; c += 32) {
+                        float v[16];
+                        if (empty) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                        } else {
+                            tmem_ld16(d + h * p.most + c, v);
+                        }
+                        if (f < p.F) {
+                            st_vec(out + c, pack8(v));
+                            if (c + 8 < cols) st_vec(out + c + 8, pack8(v + 8));
+                        }
+                    }
+                }
+            } else {
+                for (int h = 0; h < 2; ++h) {
+                    const int f = t.f0 + h * 128 + quarter * 32 + (lane & 3) * 8;
+                    if (f - (lane & 3) * 8 >= p.F) break;
+                    float bias[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+                    if (p.bias && f < p.F) unpack8(ld_vec(p.bias + (int64_t)t.e * p.F + f), bias);
+                    for (int c = group * 16; c < t.rows; c += 32) {
+                        float v[16];
+                        tmem_ld16(d + h * p.most + c, v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) tile[i * kStagePitch + lane] = v[i];
+                        __syncwarp();
+                        const float* at = tile + (lane >> 2) * kStagePitch + (lane & 3) * 8;
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4)
+                            *reinterpret_cast<float4*>(v + i) = *reinterpret_cast<const float4*>(at + (i >> 3) * 8 * kStagePitch + (i & 7));
+                        __syncwarp();
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const int r = c + half * 8 + (lane >> 2);
+                            if (r >= t.rows || f >= p.F) continue;
+                            const int64_t row = t.row + r, place = row * p.F + f;
+                            float z[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) z[i] = v[half * 8 + i] + bias[i];
+                            if (p.pre) st_vec(p.pre + place, pack8(z));
+                            if (p.act)
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) z[i] = act_value(z[i], p.act);
+                            if (p.row_scale) {
+                                const float scale = ld_plain(p.row_scale + row);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) z[i] *= scale;
+                            }
+                            if (p.residual) {
+                                float add[8];
+                                unpack8(ld_vec(p.residual + place), add);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) z[i] += add[i];
+                            }
+                            st_vec(p.out + place, pack8(z));
+                        }
+                    }
+                }
+            }
+            if (!empty) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
+                if (++acc == p.accs) {
+                    acc = 0;
+                    acc_phase ^= 1;
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    griddep_launch();
+    if (warp == 1) tmem_free<CG>(tmem, kColumns);
+}
+
+// ------------------------------------------------------------------------------------------ passes over the rows
+
+constexpr int kRowThreads = 256;
+
+// Rows quantised by an FP8 dispatch as bf16: e4m3 times the scale of its 128 channels, rounded once.  One block takes every
+// gridDim.x-th row of an expert.
+__global__ void __launch_bounds__(kRowThreads) widen_kernel(const uint8_t* q, const float* scale, uint16_t* out, int H, Segments seg) {
+    griddep_wait();
+    int first, rows;
+    for (int e = blockIdx.y; e < seg.E; e += gridDim.y) {
+        segment(seg, e, first, rows);
+        for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+            const int64_t row = first + r;
+            for (int c = threadIdx.x * 16; c < H; c += kRowThreads * 16) {
+                const uint4 in = *reinterpret_cast<const uint4*>(q + row * H + c);
+                const float s = ld_plain(scale + row * (H / 128) + c / 128);
+                const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+                float f[16];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+                    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                    f[2 * i] = v.x * s;
+                    f[2 * i + 1] = v.y * s;
+                }
+                st_vec(out + row * H + c, pack8(f));
+                st_vec(out + row * H + c + 8, pack8(f + 8));
+            }
+        }
+    }
+}
+
+// dg = dh u act'(g), du = dh act(g); pre and grad_pre may be the same array.
+__global__ void __launch_bounds__(kRowThreads) gated_grad_kernel(const uint16_t* grad, const uint16_t* pre, uint16_t* grad_pre, int I,
+                                                                int act, Segments seg) {
+    griddep_wait();
+    int first, rows;
+    for (int e = blockIdx.y; e < seg.E; e += gridDim.y) {
+        segment(seg, e, first, rows);
+        for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+            const int64_t row = first + r;
+            for (int c = threadIdx.x * 8; c < I; c += kRowThreads * 8) {
+                float dh[8], g[8], u[8];
+                unpack8(ld_vec(grad + row * I + c), dh);
+                unpack8(ld_vec(pre + row * 2 * I + c), g);
+                unpack8(ld_vec(pre + (row * 2 + 1) * I + c), u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float value, slope;
+                    act_both(g[i], act, value, slope);
+                    g[i] = dh[i] * u[i] * slope;
+                    u[i] = dh[i] * value;
+                }
+                st_vec(grad_pre + row * 2 * I + c, pack8(g));
+                st_vec(grad_pre + (row * 2 + 1) * I + c, pack8(u));
+            }
+        }
+    }
+}
+
+// dz = scale grad act'(z), and the row weight's gradient <grad, act(z)>.
+__global__ void __launch_bounds__(kRowThreads) linear_grad_kernel(const uint16_t* grad, const uint16_t* pre, const float* row_scale,
+                                                                 uint16_t* grad_pre, float* grad_scale, int N, int act, Segments seg) {
+    __shared__ float part[kRowThreads / 32];
+    griddep_wait();
+    int first, rows;
+    for (int e = blockIdx.y; e < seg.E; e += gridDim.y) {
+        segment(seg, e, first, rows);
+        for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+            const int64_t row = first + r;
+            const float scale = row_scale ? ld_plain(row_scale + row) : 1.0f;
+            float sum = 0.0f;
+            for (int c = threadIdx.x * 8; c < N; c += kRowThreads * 8) {
+                float dy[8], z[8];
+                unpack8(ld_vec(grad + row * N + c), dy);
+                unpack8(ld_vec(pre + row * N + c), z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float value, slope;
+                    act_both(z[i], act, value, slope);
+                    sum += dy[i] * value;
+                    z[i] = dy[i] * slope * scale;
+                }
+                st_vec(grad_pre + row * N + c, pack8(z));
+            }
+            if (!grad_scale) continue;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                float all = 0.0f;
+                for (int i = 0; i < kRowThreads / 32; ++i) all += part[i];
+                grad_scale[row] = all;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// The bias's gradient: dz summed over the expert's rows, in 32 bits and from dz as it is before it is rounded.  One block per 256
+// columns of an expert: a warp takes every eighth row, then the warps' sums are joined in order.
+__global__ void __launch_bounds__(kRowThreads) bias_grad_kernel(const uint16_t* grad, const uint16_t* pre, const float* row_scale,
+                                                               uint16_t* grad_bias, int N, int act, Segments seg) {
+    __shared__ float part[kRowThreads / 32][256];
+    griddep_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 256 + lane * 8;
+    int first, rows;
+    for (int e = blockIdx.y; e < seg.E; e += gridDim.y) {
+        segment(seg, e, first, rows);
+        float sum[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+        if (c < N)
+            for (int r = warp; r < rows; r += kRowThreads / 32) {
+                const int64_t row = first + r;
+                const float scale = row_scale ? ld_plain(row_scale + row) : 1.0f;
+                float dy[8], z[8];
+                unpack8(ld_vec(grad + row * N + c), dy);
+                if (act) {
+                    unpack8(ld_vec(pre + row * N + c), z);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float value, slope;
+                        act_both(z[i], act, value, slope);
+                        dy[i] *= slope;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += dy[i] * scale;
+            }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[warp][lane * 8 + i] = sum[i];
+        __syncthreads();
+        const int col = blockIdx.x * 256 + threadIdx.x;
+        if (col < N) {
+            float all = 0.0f;
+            for (int w = 0; w < kRowThreads / 32; ++w) all += part[w][threadIdx.x];
+            const __nv_bfloat16 v = __float2bfloat16_rn(all);
+            grad_bias[(int64_t)e * N + col] = *reinterpret_cast<const uint16_t*>(&v);
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------ host
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder() {
+    static std::atomic<void*> fn{nullptr};
+    void* f = fn.load(std::memory_order_acquire);
+    if (!f) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        fn.store(f, std::memory_order_release);
+    }
+    return reinterpret_cast<EncodeFn>(f);
+}
+
+// bf16 [planes, rows, cols], boxes of `box_rows` x 64, 128-byte swizzle; what lies outside reads as zero.
+bool make_map(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t planes, unsigned box_rows) {
+    const EncodeFn encode = encoder();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {cols, rows, planes}, strides[2] = {cols * 2, cols * rows * 2};
+    const cuuint32_t box[3] = {64, box_rows, 1}, steps[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct DeviceFacts {
+    int sms = 0, smem = 0;
+};
+cudaError_t device_facts(DeviceFacts* f) {
+    static std::atomic<uint64_t> known[kAttrDevices];   // what a device is does not change: SMs and shared memory, packed
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t v = dev < kAttrDevices ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (v) {
+        f->sms = (int)(v >> 32);
+        f->smem = (int)(v & 0xffffffffu);
+        return cudaSuccess;
+    }
+    e = cudaDeviceGetAttribute(&f->sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&f->smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
+    if (e == cudaSuccess && dev < kAttrDevices) known[dev].store(((uint64_t)f->sms << 32) | (uint32_t)f->smem, std::memory_order_relaxed);
+    return e;
+}
+
+template <int MODE>
+cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, Product p, cudaStream_t st) {
+    DeviceFacts dev;
+    cudaError_t e = device_facts(&dev);
+    if (e != cudaSuccess) return e;
+    p.stage_bytes = 2 * kHalfBytes + p.most * 128;
+    p.accs = 4 * p.most <= kColumns ? 2 : 1;
+    const int tiles = kResultWarps * kStageFloats * 4;
+    const int room = dev.smem - 1024 - (int)sizeof(Shared) - tiles;
+    p.stages = room / p.stage_bytes;
+    if (p.stages > kMaxRing) p.stages = kMaxRing;
+    if (p.stages < 2) return cudaErrorInvalidConfiguration;
+    const int smem = p.stages * p.stage_bytes + tiles + 1024;
+    static std::atomic<int> granted[kAttrDevices];
+    e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, 1>), smem, granted);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(expert_kernel<MODE, 1>, dev.sms, kGemmThreads, (size_t)smem, st, false, 1, a, b, p);
+}
+
+// Rows per tile: the segments of a call are not known to the host, their capacity is.  Small pieces leave room for more stages
+// and a second accumulator.
+int rows_per_tile(const ubep_expert_rows_t& r) {
+    const int64_t each = (int64_t)r.num_ranks * r.rows_per_rank_cap / r.num_experts;
+    return each <= 64 ? 64 : each <= 128 ? 128 : 256;
+}
+
+dim3 row_grid(const ubep_expert_rows_t& r, const DeviceFacts& dev) {
+    const int per = (dev.sms * 16 + r.num_experts - 1) / r.num_experts;
+    return dim3((unsigned)(per < r.rows_per_rank_cap ? per : r.rows_per_rank_cap), (unsigned)(r.num_experts < 65535 ? r.num_experts : 65535));
+}
+
+Segments segments_of(const ubep_expert_rows_t& r) {
+    return Segments{r.offset, r.count, r.num_experts, r.num_experts / r.num_ranks, r.rows_per_rank_cap};
+}
+
+// x as bf16 rows: itself, or widened into the scratch.
+cudaError_t rows_in(const ubep_expert_rows_t& r, const void* x, const float* x_scale, void* scratch, int K, const void** out,
+                    cudaStream_t st, int* launches) {
+    *out = x;
+    if (!x_scale) return cudaSuccess;
+    DeviceFacts dev;
+    cudaError_t e = device_facts(&dev);
+    if (e != cudaSuccess) return e;
+    dim3 grid = row_grid(r, dev);
+    widen_kernel<<<grid, kRowThreads, 0, st>>>(static_cast<const uint8_t*>(x), x_scale, static_cast<uint16_t*>(scratch), K, segments_of(r));
+    *out = scratch;
+    ++*launches;
+    return cudaGetLastError();
+}
+
+uint64_t all_rows(const ubep_expert_rows_t& r) { return (uint64_t)r.num_ranks * r.rows_per_rank_cap; }
+
+// dx[row, k] = sum_n dz[row, n] w[e, n, k]
+cudaError_t rows_grad(const ubep_expert_rows_t& r, const void* dz, const void* w, int K, int N, void* grad_x, cudaStream_t st) {
+    Product p{};
+    p.seg = segments_of(r);
+    p.F = K;
+    p.K = N;
+    p.most = rows_per_tile(r);
+    p.out = static_cast<uint16_t*>(grad_x);
+    p.status = r.status;
+    CUtensorMap a, b;
+    if (!make_map(&a, w, K, N, r.num_experts, 64) || !make_map(&b, dz, N, all_rows(r), 1, 32)) return cudaErrorInvalidValue;
+    return launch_product<kRowsGrad>(a, b, p, st);
+}
+
+// dw[e, n, k] = sum_row dz[row, n] x[row, k]
+cudaError_t weights_grad(const ubep_expert_rows_t& r, const void* dz, const void* x, int K, int N, void* grad_w, cudaStream_t st) {
+    Product p{};
+    p.seg = segments_of(r);
+    p.F = N;
+    p.FB = K;
+    p.most = 256;
+    p.out = static_cast<uint16_t*>(grad_w);
+    p.status = r.status;
+    CUtensorMap a, b;
+    if (!make_map(&a, dz, N, all_rows(r), 1, 64) || !make_map(&b, x, K, all_rows(r), 1, 64)) return cudaErrorInvalidValue;
+    return launch_product<kWeightsGrad>(a, b, p, st);
+}
+
+}  // namespace
+
+cudaError_t launch_expert_gated(const ubep_expert_rows_t& r, const void* x, const float* x_scale, const void* w, int H, int I, int act,
+                                void* h, void* pre, void* scratch, cudaStream_t st, int* launches) {
+    const void* rows;
+    cudaError_t e = rows_in(r, x, x_scale, scratch, H, &rows, st, launches);
+    if (e != cudaSuccess) return e;
+    Product p{};
+    p.seg = segments_of(r);
+    p.F = I;
+    p.K = H;
+    p.most = rows_per_tile(r);
+    p.act = act;
+    p.out = static_cast<uint16_t*>(h);
+    p.pre = static_cast<uint16_t*>(pre);
+    p.status = r.status;
+    CUtensorMap a, b;
+    if (!make_map(&a, w, H, I, 2 * (uint64_t)r.num_experts, 128) || !make_map(&b, rows, H, all_rows(r), 1, 32)) return cudaErrorInvalidValue;
+    e = launch_product<kGated>(a, b, p, st);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+cudaError_t launch_expert_gated_backward(const ubep_expert_rows_t& r, const void* x, const float* x_scale, const void* w, const void* pre,
+                                         const void* grad_h, int H, int I, int act, void* grad_pre, void* grad_x, void* grad_w,
+                                         void* scratch, cudaStream_t st, int* launches) {
+    const void* rows;
+    cudaError_t e = rows_in(r, x, grad_w ? x_scale : nullptr, scratch, H, &rows, st, launches);
+    if (e != cudaSuccess) return e;
+    DeviceFacts dev;
+    e = device_facts(&dev);
+    if (e != cudaSuccess) return e;
+    gated_grad_kernel<<<row_grid(r, dev), kRowThreads, 0, st>>>(static_cast<const uint16_t*>(grad_h), static_cast<const uint16_t*>(pre),
+                                                               static_cast<uint16_t*>(grad_pre), I, act, segments_of(r));
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    if (grad_x) {
+        e = rows_grad(r, grad_pre, w, H, 2 * I, grad_x, st);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    if (grad_w) {
+        e = weights_grad(r, grad_pre, rows, H, 2 * I, grad_w, st);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    return cudaSuccess;
+}
+
+cudaError_t launch_expert_linear(const ubep_expert_rows_t& r, const void* x, const void* w, const void* bias, const float* row_scale,
+                                 const void* residual, int K, int N, int act, void* y, void* pre, cudaStream_t st, int* launches) {
+    Product p{};
+    p.seg = segments_of(r);
+    p.F = N;
+    p.K = K;
+    p.most = rows_per_tile(r);
+    p.act = act;
+    p.out = static_cast<uint16_t*>(y);
+    p.pre = static_cast<uint16_t*>(pre);
+    p.bias = static_cast<const uint16_t*>(bias);
+    p.residual = static_cast<const uint16_t*>(residual);
+    p.row_scale = row_scale;
+    p.status = r.status;
+    CUtensorMap a, b;
+    if (!make_map(&a, w, K, N, r.num_experts, 128) || !make_map(&b, x, K, all_rows(r), 1, 32)) return cudaErrorInvalidValue;
+    const cudaError_t e = launch_product<kLinear>(a, b, p, st);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
+cudaError_t launch_expert_linear_backward(const ubep_expert_rows_t& r, const void* x, const void* w, const void* pre,
+                                          const float* row_scale, const void* grad_y, int K, int N, int act, void* grad_pre,
+                                          void* grad_x, void* grad_w, void* grad_bias, float* grad_scale, cudaStream_t st,
+                                          int* launches) {
+    DeviceFacts dev;
+    cudaError_t e = device_facts(&dev);
+    if (e != cudaSuccess) return e;
+    const void* dz = grad_y;
+    if (act || row_scale) {
+        linear_grad_kernel<<<row_grid(r, dev), kRowThreads, 0, st>>>(static_cast<const uint16_t*>(grad_y), static_cast<const uint16_t*>(pre),
+                                                                    row_scale, static_cast<uint16_t*>(grad_pre), grad_scale, N, act,
+                                                                    segments_of(r));
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        ++*launches;
+        dz = grad_pre;
+    }
+    if (grad_bias) {
+        const dim3 grid((unsigned)((N + 255) / 256), (unsigned)(r.num_experts < 65535 ? r.num_experts : 65535));
+        bias_grad_kernel<<<grid, kRowThreads, 0, st>>>(static_cast<const uint16_t*>(grad_y), static_cast<const uint16_t*>(pre), row_scale,
+                                                      static_cast<uint16_t*>(grad_bias), N, act, segments_of(r));
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    if (grad_x) {
+        e = rows_grad(r, dz, w, K, N, grad_x, st);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    if (grad_w) {
+        e = weights_grad(r, dz, x, K, N, grad_w, st);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace ubep

@@ -1,0 +1,107 @@
+// The expert products' arithmetic and the walk over ragged segments, shared by their kernels.
+#pragma once
+
+#include "ubep_common.cuh"
+
+namespace ubep {
+
+enum { kActNone = 0, kActSilu = 1, kActGelu = 2, kActRelu = 3 };
+
+// Sums and activations are taken in 32 bits; expf and the quotient may be off by a few units of 2^-23, far inside the half
+// step (2^-9) of the bf16 results.
+__device__ __forceinline__ float act_value(float z, int act) {
+    if (act == kActSilu) return __fdividef(z, 1.0f + __expf(-z));
+    if (act == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    if (act == kActRelu) return z > 0.0f || z != z ? z : 0.0f;
+    return z;
+}
+// The value and the derivative.
+__device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
+    if (act == kActSilu) {
+        const float p = __fdividef(1.0f, 1.0f + __expf(-z));
+        value = z * p;
+        slope = p * (1.0f + z * (1.0f - p));
+    } else if (act == kActGelu) {
+        const float c = 0.5f * (1.0f + erff(z * 0.70710678f));
+        value = z * c;
+        slope = c + z * __expf(-0.5f * z * z) * 0.39894228f;
+    } else if (act == kActRelu) {
+        value = z > 0.0f || z != z ? z : 0.0f;
+        slope = z > 0.0f ? 1.0f : 0.0f;
+    } else {
+        value = z;
+        slope = 1.0f;
+    }
+}
+
+__device__ __forceinline__ void unpack8(const uint4 in, float* f) {
+    const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+}
+
+// The experts' segments.  Whatever the arrays hold, a segment lies inside its region.
+struct Segments {
+    const int32_t *offset, *count;
+    int E, L, cap;   // experts, experts per region, rows per region
+};
+__device__ __forceinline__ void segment(const Segments& s, int e, int& first, int& rows) {
+    first = min(max(ld_plain(s.offset + e), 0), s.cap);
+    rows = min(max(ld_plain(s.count + e), 0), s.cap - first);
+    first += e / s.L * s.cap;
+}
+
+// Tiles of one expert: `rows` rows cut into equal pieces of at most `most`, the pieces whole multiples of `unit` rows.
+__device__ __forceinline__ int row_tiles(int rows, int most) { return (rows + most - 1) / most; }
+
+// Walks the experts' tiles in order, 32 experts at a time; every lane of a converged warp takes part.  Tile numbers only grow.
+struct TileWalk {
+    int base, before;          // first expert of the window, tiles in front of it
+    int first, rows, upto;     // this lane's expert: its segment, tiles of the window up to and with it
+    __device__ __forceinline__ void load(const Segments& s, int per_row_tile, int most, bool every) {
+        const int lane = threadIdx.x & 31, e = base + lane;
+        first = rows = 0;
+        int n = 0;
+        if (e < s.E) {
+            segment(s, e, first, rows);
+            n = every ? per_row_tile : row_tiles(rows, most) * per_row_tile;
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, n, o);
+            if (lane >= o) n += u;
+        }
+        upto = n;
+    }
+    // Tile t: its expert, segment and place among the expert's tiles; false behind the last one.
+    __device__ __forceinline__ bool find(const Segments& s, int per_row_tile, int most, bool every, int t, int& e, int& seg_first,
+                                         int& seg_rows, int& place) {
+        for (;;) {
+            const int all = __shfl_sync(0xffffffffu, upto, 31);
+            if (t < before + all) break;
+            before += all;
+            base += 32;
+            if (base >= s.E) return false;
+            load(s, per_row_tile, most, every);
+        }
+        const int src = __ffs(__ballot_sync(0xffffffffu, t < before + upto)) - 1;
+        const int in_front = __shfl_sync(0xffffffffu, upto, max(src - 1, 0));
+        e = base + src;
+        seg_first = __shfl_sync(0xffffffffu, first, src);
+        seg_rows = __shfl_sync(0xffffffffu, rows, src);
+        place = t - before - (src ? in_front : 0);
+        return true;
+    }
+};
+
+}  // namespace ubep

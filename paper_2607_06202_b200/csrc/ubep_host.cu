@@ -5,6 +5,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <string>
 #include <vector>
@@ -13,6 +14,7 @@
 #include "ubep_kernels.h"
 #include "ubep_sync.h"
 #include "ubep_sharded.h"
+#include "ubep_experts.h"
 
 using ubep::Params;
 
@@ -448,6 +450,47 @@ struct DeviceGuard {
     }
 };
 
+bool route_args(const void* logits, int type, const void* idx, const void* w, int32_t T, int32_t E, int32_t k) {
+    if (type != UBEP_LOGITS_F32 && type != UBEP_LOGITS_BF16) return false;
+    if (T < 0 || E < 1 || E > 65535 || k < 1 || k > ubep::kMaxTopk) return false;
+    if (T > 0 && (!logits || !idx || !w)) return false;
+    return aligned16(logits) && aligned16(idx) && aligned16(w);
+}
+
+// All there must be, and on a 16-byte boundary.
+bool arrays(std::initializer_list<const void*> needed, std::initializer_list<const void*> optional) {
+    for (const void* p : needed)
+        if (!p || !aligned16(p)) return false;
+    for (const void* p : optional)
+        if (!aligned16(p)) return false;
+    return true;
+}
+
+bool expert_args(const ubep_expert_rows_t* r, int32_t in, int32_t out, int act) {
+    if (!r || !r->offset || !r->count || r->num_experts < 1 || r->num_ranks < 1 || r->num_experts % r->num_ranks != 0) return false;
+    if (r->rows_per_rank_cap < 1 || (int64_t)r->num_ranks * r->rows_per_rank_cap > INT32_MAX) return false;
+    if (r->num_experts > 65535 || r->device < 0) return false;
+    // (1 << 28 features: a tensor map's strides stay below its limit, and feature numbers in 32 bits)
+    if (in < 8 || out < 8 || in % 8 != 0 || out % 8 != 0 || in > (1 << 20) || out > (1 << 20)) return false;
+    return act >= UBEP_ACT_NONE && act <= UBEP_ACT_RELU;
+}
+
+// Runs `launch` on the device of the call; a refused launch leaves no error behind for the caller's next check.
+template <typename F>
+int on_device(int device, F launch) {
+    DeviceGuard guard(device);
+    if (guard.err != cudaSuccess) {
+        cudaGetLastError();
+        return UBEP_ERR_CUDA;
+    }
+    int launches = 0;
+    const cudaError_t e = launch(&launches);
+    g_launches += launches;
+    if (e == cudaSuccess) return UBEP_OK;
+    cudaGetLastError();
+    return UBEP_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
@@ -848,6 +891,88 @@ int ubep_combine_sharded(ubep_buffer_t* buf, const void* const* y_peers, const f
     if (e != cudaSuccess) return cuda_fail(buf, e);
     g_launches += 1;
     return UBEP_OK;
+}
+
+// ------------------------------------------------------------------ router and experts
+
+int ubep_route(const void* logits, int logits_type, int32_t T, int32_t E, int32_t k, int32_t renormalize, int32_t* topk_idx,
+               float* topk_w, int32_t device, void* cuda_stream) {
+    if (!route_args(logits, logits_type, topk_idx, topk_w, T, E, k)) return UBEP_ERR_ARG;
+    if (T == 0) return UBEP_OK;
+    return on_device(device, [&](int* n) {
+        *n = 1;
+        return ubep::launch_route(logits, logits_type, T, E, k, renormalize != 0, topk_idx, topk_w, static_cast<cudaStream_t>(cuda_stream));
+    });
+}
+
+int ubep_route_backward(const void* logits, int logits_type, const int32_t* topk_idx, const float* grad_w, int32_t T, int32_t E, int32_t k,
+                        int32_t renormalize, void* grad_logits, int32_t device, void* cuda_stream) {
+    if (!route_args(logits, logits_type, topk_idx, grad_w, T, E, k)) return UBEP_ERR_ARG;
+    if (T == 0) return UBEP_OK;
+    if (!grad_logits || !aligned16(grad_logits) || grad_logits == logits) return UBEP_ERR_ARG;
+    return on_device(device, [&](int* n) {
+        *n = 1;
+        return ubep::launch_route_backward(logits, logits_type, topk_idx, grad_w, T, E, k, renormalize != 0, grad_logits,
+                                           static_cast<cudaStream_t>(cuda_stream));
+    });
+}
+
+int ubep_expert_rows(ubep_buffer_t* buf, ubep_expert_rows_t* rows) {
+    if (!buf || !rows || buf->cfg.dedup) return UBEP_ERR_ARG;
+    const ubep_config_t& c = buf->cfg;
+    const bool one = buf->my_rank >= 0;   // sharded use: this rank's experts
+    const int L = c.num_experts / c.num_ranks;
+    rows->offset = at<int32_t>(buf, buf->lay.off[UBEP_VIEW_EXPERT_OFFSET]) + (one ? buf->my_rank * L : 0);
+    rows->count = at<int32_t>(buf, buf->lay.off[UBEP_VIEW_NUM_TOKENS_PER_EXPERT]) + (one ? buf->my_rank * L : 0);
+    rows->num_experts = one ? L : c.num_experts;
+    rows->num_ranks = one ? 1 : c.num_ranks;
+    rows->rows_per_rank_cap = c.rows_per_rank_cap;
+    rows->device = c.device;
+    rows->status = at<int32_t>(buf, buf->lay.status);
+    return UBEP_OK;
+}
+
+int ubep_expert_gated(const ubep_expert_rows_t* rows, const void* x, const float* x_scale, const void* w, int32_t H, int32_t I, int act,
+                      void* h, void* pre, void* scratch, void* cuda_stream) {
+    if (!expert_args(rows, H, I, act) || !arrays({x, w, h}, {x_scale, pre, scratch})) return UBEP_ERR_ARG;
+    if (x_scale && (H % 128 != 0 || !scratch)) return UBEP_ERR_ARG;
+    return on_device(rows->device, [&](int* n) {
+        return ubep::launch_expert_gated(*rows, x, x_scale, w, H, I, act, h, pre, scratch, static_cast<cudaStream_t>(cuda_stream), n);
+    });
+}
+
+int ubep_expert_gated_backward(const ubep_expert_rows_t* rows, const void* x, const float* x_scale, const void* w, const void* pre,
+                               const void* grad_h, int32_t H, int32_t I, int act, void* grad_pre, void* grad_x, void* grad_w,
+                               void* scratch, void* cuda_stream) {
+    if (!expert_args(rows, H, I, act) || !arrays({pre, grad_h, grad_pre}, {x, w, x_scale, grad_x, grad_w, scratch})) return UBEP_ERR_ARG;
+    if ((grad_x && !w) || (grad_w && !x) || (!grad_x && !grad_w)) return UBEP_ERR_ARG;
+    if (grad_w && x_scale && (H % 128 != 0 || !scratch)) return UBEP_ERR_ARG;
+    return on_device(rows->device, [&](int* n) {
+        return ubep::launch_expert_gated_backward(*rows, x, x_scale, w, pre, grad_h, H, I, act, grad_pre, grad_x, grad_w, scratch,
+                                                  static_cast<cudaStream_t>(cuda_stream), n);
+    });
+}
+
+int ubep_expert_linear(const ubep_expert_rows_t* rows, const void* x, const void* w, const void* bias, const float* row_scale,
+                       const void* residual, int32_t K, int32_t N, int act, void* y, void* pre, void* cuda_stream) {
+    if (!expert_args(rows, K, N, act) || !arrays({x, w, y}, {bias, row_scale, residual, pre})) return UBEP_ERR_ARG;
+    return on_device(rows->device, [&](int* n) {
+        return ubep::launch_expert_linear(*rows, x, w, bias, row_scale, residual, K, N, act, y, pre, static_cast<cudaStream_t>(cuda_stream), n);
+    });
+}
+
+int ubep_expert_linear_backward(const ubep_expert_rows_t* rows, const void* x, const void* w, const void* pre, const float* row_scale,
+                                const void* grad_y, int32_t K, int32_t N, int act, void* grad_pre, void* grad_x, void* grad_w,
+                                void* grad_bias, float* grad_row_scale, void* cuda_stream) {
+    if (!expert_args(rows, K, N, act) || !arrays({grad_y}, {x, w, pre, row_scale, grad_pre, grad_x, grad_w, grad_bias, grad_row_scale}))
+        return UBEP_ERR_ARG;
+    if ((grad_x && !w) || (grad_w && !x) || (grad_row_scale && !row_scale)) return UBEP_ERR_ARG;
+    if ((act != UBEP_ACT_NONE || row_scale) && (!pre || !grad_pre || (grad_pre == pre && grad_bias))) return UBEP_ERR_ARG;
+    if (!grad_x && !grad_w && !grad_bias && !grad_row_scale) return UBEP_ERR_ARG;
+    return on_device(rows->device, [&](int* n) {
+        return ubep::launch_expert_linear_backward(*rows, x, w, pre, row_scale, grad_y, K, N, act, grad_pre, grad_x, grad_w, grad_bias,
+                                                   grad_row_scale, static_cast<cudaStream_t>(cuda_stream), n);
+    });
 }
 
 int ubep_view(ubep_buffer_t* buf, int which, void** dev_ptr, int64_t shape[4]) {

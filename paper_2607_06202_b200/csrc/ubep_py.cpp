@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <cstdio>
 #include <exception>
 
 #include "../../include/ubep.h"
@@ -26,6 +27,12 @@ decltype(&ubep_dispatch) f_dispatch;
 decltype(&ubep_combine) f_combine;
 decltype(&ubep_get_dispatch_layout) f_layout;
 decltype(&ubep_dispatch_sync) f_dispatch_sync;
+decltype(&ubep_route) f_route;
+decltype(&ubep_route_backward) f_route_backward;
+decltype(&ubep_expert_gated) f_gated;
+decltype(&ubep_expert_gated_backward) f_gated_backward;
+decltype(&ubep_expert_linear) f_linear;
+decltype(&ubep_expert_linear_backward) f_linear_backward;
 
 // An argument that must be a contiguous tensor, or None where the C ABI takes a null pointer.
 bool tensor_arg(PyObject* o, void** ptr, const at::Tensor** t = nullptr) {
@@ -262,6 +269,337 @@ PyObject* py_layout_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
 }
 
+// ------------------------------------------------------------------ router and experts
+//
+// These calls take their sizes from the tensors, so they hold every tensor against them: a wrong type or shape raises a
+// ValueError that names the argument, and nothing is launched.
+
+struct Refused : std::exception {
+    char text[160];
+    Refused(const char* name, const char* what) { std::snprintf(text, sizeof text, "%s: %s", name, what); }
+    const char* what() const noexcept override { return text; }
+};
+struct Raised : std::exception {};   // the Python error is set
+
+PyObject* refused_or_raised() {
+    try {
+        throw;
+    } catch (const Raised&) {
+    } catch (const Refused& e) {
+        PyErr_SetString(PyExc_ValueError, e.what());
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    return nullptr;
+}
+
+// Where the tensors of a call live and which stream it runs on; temporaries are tied to that stream.
+struct Place {
+    c10::Device dev{c10::kCUDA, 0};
+    void* stream = nullptr;
+    bool foreign = false;   // not torch's current stream
+    explicit Place(const at::Tensor& any, PyObject* s) : dev(any.device()) {
+        const auto current = c10::cuda::getCurrentCUDAStream(dev.index());
+        if (s == Py_None) {
+            stream = current.stream();
+            return;
+        }
+        if (!stream_arg(s, &stream)) throw Raised();
+        foreign = stream != static_cast<void*>(current.stream());
+    }
+    at::Tensor make(c10::IntArrayRef shape, at::ScalarType type) const { return at::detail::empty_cuda(shape, type, dev, c10::nullopt); }
+    // memory of this call alone: given back when it returns, so the allocator has to know who still works on it
+    at::Tensor scratch(c10::IntArrayRef shape, at::ScalarType type) const {
+        at::Tensor t = make(shape, type);
+        if (foreign)
+            t.record_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), dev.index()).unwrap());
+        return t;
+    }
+};
+
+const at::Tensor& need(PyObject* o, const char* name) {
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s: expected a tensor, got %s", name, Py_TYPE(o)->tp_name);
+        throw Raised();
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) throw Refused(name, "not on a GPU");
+    if (!t.is_contiguous()) {
+        PyErr_SetString(PyExc_AssertionError, "tensor is not contiguous");
+        throw Raised();
+    }
+    return t;
+}
+void hold(const at::Tensor& t, const char* name, const c10::Device& dev, at::ScalarType type, c10::IntArrayRef shape) {
+    if (t.device() != dev) throw Refused(name, "on another device");
+    if (t.scalar_type() != type) throw Refused(name, "of another type than the call takes");
+    if (t.sizes() != shape) throw Refused(name, "of another shape than the other tensors ask for");
+}
+// A tensor of this type and shape, or None.
+void* maybe(PyObject* o, const char* name, const c10::Device& dev, at::ScalarType type, c10::IntArrayRef shape) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = need(o, name);
+    hold(t, name, dev, type, shape);
+    return t.data_ptr();
+}
+// An output: a tensor, or None / True = a new one, or (where the caller may do without) False.
+struct Output {
+    at::Tensor made;
+    PyObject* given = nullptr;
+    void* ptr = nullptr;
+    Output(PyObject* o, const char* name, const Place& at, at::ScalarType type, c10::IntArrayRef shape, bool none_is_new) {
+        if (o == Py_False || (o == Py_None && !none_is_new)) return;
+        if (o == Py_None || o == Py_True) {
+            made = at.make(shape, type);
+            ptr = made.data_ptr();
+        } else {
+            ptr = maybe(o, name, at.dev, type, shape);
+            given = o;
+        }
+    }
+    PyObject* result() {
+        if (given) return Py_NewRef(given);
+        if (made.defined()) return THPVariable_Wrap(std::move(made));
+        Py_RETURN_NONE;
+    }
+};
+int32_t narrow(int64_t v, const char* name) {
+    if (v > INT32_MAX) throw Refused(name, "too large");
+    return (int32_t)v;
+}
+
+int64_t number(PyObject* o) {
+    long long v;
+    if (!int_arg(o, &v)) throw Raised();
+    return v;
+}
+
+// route(logits, topk, renormalize, topk_idx, topk_w, stream): (topk_idx, topk_w), or the code
+PyObject* py_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        if (!want_args(n, 6)) return nullptr;
+        const at::Tensor& logits = need(a[0], "logits");
+        if (logits.dim() != 2) throw Refused("logits", "not [tokens, experts]");
+        const bool f32 = logits.scalar_type() == at::kFloat;
+        if (!f32 && logits.scalar_type() != at::kBFloat16) throw Refused("logits", "neither fp32 nor bf16");
+        const Place at(logits, a[5]);
+        const int64_t T = logits.size(0), k = number(a[1]);
+        if (k < 1 || k > 32) return PyLong_FromLong(UBEP_ERR_ARG);
+        const int renorm = PyObject_IsTrue(a[2]);
+        if (renorm < 0) return nullptr;
+        Output idx(a[3], "topk_idx", at, at::kInt, {T, k}, true), w(a[4], "topk_w", at, at::kFloat, {T, k}, true);
+        const void* pl = logits.data_ptr();
+        const int32_t Ti = narrow(T, "logits"), E = narrow(logits.size(1), "logits");
+        const int rc = without_gil([&] {
+            return f_route(pl, f32 ? UBEP_LOGITS_F32 : UBEP_LOGITS_BF16, Ti, E, (int32_t)k, renorm, static_cast<int32_t*>(idx.ptr),
+                           static_cast<float*>(w.ptr), at.dev.index(), at.stream);
+        });
+        if (rc != UBEP_OK) return PyLong_FromLong(rc);
+        return Py_BuildValue("(NN)", idx.result(), w.result());
+    } catch (...) {
+        return refused_or_raised();
+    }
+}
+
+// route_backward(logits, topk_idx, grad_w, renormalize, grad_logits, stream): grad_logits, or the code
+PyObject* py_route_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        if (!want_args(n, 6)) return nullptr;
+        const at::Tensor& logits = need(a[0], "logits");
+        if (logits.dim() != 2) throw Refused("logits", "not [tokens, experts]");
+        const bool f32 = logits.scalar_type() == at::kFloat;
+        if (!f32 && logits.scalar_type() != at::kBFloat16) throw Refused("logits", "neither fp32 nor bf16");
+        const Place at(logits, a[5]);
+        const at::Tensor& idx = need(a[1], "topk_idx");
+        if (idx.dim() != 2) throw Refused("topk_idx", "not [tokens, k]");
+        const int64_t T = logits.size(0), k = idx.size(1);
+        hold(idx, "topk_idx", at.dev, at::kInt, {T, k});
+        const at::Tensor& gw = need(a[2], "grad_w");
+        hold(gw, "grad_w", at.dev, at::kFloat, {T, k});
+        const int renorm = PyObject_IsTrue(a[3]);
+        if (renorm < 0) return nullptr;
+        Output out(a[4], "grad_logits", at, logits.scalar_type(), logits.sizes(), true);
+        const void* pl = logits.data_ptr();
+        const int32_t *pi = idx.data_ptr<int32_t>(), Ti = narrow(T, "logits"), E = narrow(logits.size(1), "logits");
+        const float* pg = gw.data_ptr<float>();
+        const int rc = without_gil([&] {
+            return f_route_backward(pl, f32 ? UBEP_LOGITS_F32 : UBEP_LOGITS_BF16, pi, pg, Ti, E, (int32_t)k, renorm, out.ptr, at.dev.index(),
+                                    at.stream);
+        });
+        if (rc != UBEP_OK) return PyLong_FromLong(rc);
+        return out.result();
+    } catch (...) {
+        return refused_or_raised();
+    }
+}
+
+// The first three arguments of the expert calls: offset, count, status or None; the regions are those of `x`.
+ubep_expert_rows_t rows_arg(PyObject* const* a, const Place& at, int64_t ranks, int64_t cap) {
+    const at::Tensor &offset = need(a[0], "offset"), &count = need(a[1], "count");
+    if (offset.dim() != 1) throw Refused("offset", "not [experts]");
+    hold(offset, "offset", at.dev, at::kInt, {offset.size(0)});
+    hold(count, "count", at.dev, at::kInt, {offset.size(0)});
+    ubep_expert_rows_t r{};
+    r.offset = offset.data_ptr<int32_t>();
+    r.count = count.data_ptr<int32_t>();
+    r.num_experts = narrow(offset.size(0), "offset");
+    r.num_ranks = narrow(ranks, "x");
+    r.rows_per_rank_cap = narrow(cap, "x");
+    r.device = at.dev.index();
+    r.status = static_cast<int32_t*>(maybe(a[2], "status", at.dev, at::kInt, {1}));
+    return r;
+}
+
+// Rows with their scales or without: [ranks, cap, width].
+struct RowsIn {
+    const at::Tensor& t;
+    int64_t R, cap, width;
+    void* scale = nullptr;
+    RowsIn(PyObject* x, PyObject* x_scale) : t(need(x, "x")) {
+        if (t.dim() != 3) throw Refused("x", "not [ranks, rows, width]");
+        R = t.size(0), cap = t.size(1), width = t.size(2);
+        const auto type = t.scalar_type();
+        if (x_scale != Py_None) {
+            if (type != at::kFloat8_e4m3fn && type != at::kByte) throw Refused("x", "rows with scales are e4m3");
+            if (width % 128 != 0) throw Refused("x", "rows with scales have a multiple of 128 channels");
+            scale = maybe(x_scale, "x_scale", t.device(), at::kFloat, {R, cap, width / 128});
+        } else if (type == at::kByte) {   // a receive region as the buffer's view shows it
+            if (width % 2 != 0) throw Refused("x", "rows of bf16 have an even number of bytes");
+            width /= 2;
+        } else if (type != at::kBFloat16) {
+            throw Refused("x", "neither bf16 rows nor e4m3 rows with scales");
+        }
+    }
+};
+
+// expert_gated(offset, count, status, x, x_scale, w, act, out, pre, stream): out, or the code
+PyObject* py_gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        if (!want_args(n, 10)) return nullptr;
+        const RowsIn x(a[3], a[4]);
+        const Place at(x.t, a[9]);
+        const ubep_expert_rows_t r = rows_arg(a, at, x.R, x.cap);
+        const at::Tensor& w = need(a[5], "w");
+        if (w.dim() != 4) throw Refused("w", "not [experts, 2, inner, width]");
+        const int64_t I = w.size(2);
+        hold(w, "w", at.dev, at::kBFloat16, {(int64_t)r.num_experts, 2, I, x.width});
+        const int act = (int)number(a[6]);
+        Output out(a[7], "out", at, at::kBFloat16, {x.R, x.cap, I}, true);
+        void* pre = maybe(a[8], "pre", at.dev, at::kBFloat16, {x.R, x.cap, 2, I});
+        at::Tensor scratch;
+        if (x.scale) scratch = at.scratch({x.R, x.cap, x.width}, at::kBFloat16);
+        const void *px = x.t.data_ptr(), *pw = w.data_ptr();
+        void* ps = x.scale ? scratch.data_ptr() : nullptr;
+        const int32_t H = narrow(x.width, "x"), Ii = narrow(I, "w");
+        const int rc = without_gil([&] { return f_gated(&r, px, static_cast<const float*>(x.scale), pw, H, Ii, act, out.ptr, pre, ps, at.stream); });
+        if (rc != UBEP_OK) return PyLong_FromLong(rc);
+        return out.result();
+    } catch (...) {
+        return refused_or_raised();
+    }
+}
+
+// expert_gated_backward(offset, count, status, x, x_scale, w, pre, grad_h, act, grad_pre, grad_x, grad_w, stream): (grad_x, grad_w), or the code
+PyObject* py_gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        if (!want_args(n, 13)) return nullptr;
+        const RowsIn x(a[3], a[4]);
+        const Place at(x.t, a[12]);
+        const ubep_expert_rows_t r = rows_arg(a, at, x.R, x.cap);
+        const at::Tensor& w = need(a[5], "w");
+        if (w.dim() != 4) throw Refused("w", "not [experts, 2, inner, width]");
+        const int64_t I = w.size(2);
+        hold(w, "w", at.dev, at::kBFloat16, {(int64_t)r.num_experts, 2, I, x.width});
+        const at::Tensor &pre = need(a[6], "pre"), &gh = need(a[7], "grad_h");
+        hold(pre, "pre", at.dev, at::kBFloat16, {x.R, x.cap, 2, I});
+        hold(gh, "grad_h", at.dev, at::kBFloat16, {x.R, x.cap, I});
+        const int act = (int)number(a[8]);
+        at::Tensor room, scratch;
+        void* gp = maybe(a[9], "grad_pre", at.dev, at::kBFloat16, {x.R, x.cap, 2, I});
+        if (!gp) {
+            room = at.scratch({x.R, x.cap, 2, I}, at::kBFloat16);
+            gp = room.data_ptr();
+        }
+        Output gx(a[10], "grad_x", at, at::kBFloat16, {x.R, x.cap, x.width}, true), gw(a[11], "grad_w", at, at::kBFloat16, w.sizes(), true);
+        if (x.scale && gw.ptr) scratch = at.scratch({x.R, x.cap, x.width}, at::kBFloat16);
+        const void *px = x.t.data_ptr(), *pw = w.data_ptr(), *pp = pre.data_ptr(), *ph = gh.data_ptr();
+        void* ps = scratch.defined() ? scratch.data_ptr() : nullptr;
+        const int32_t H = narrow(x.width, "x"), Ii = narrow(I, "w");
+        const int rc = without_gil([&] {
+            return f_gated_backward(&r, px, static_cast<const float*>(x.scale), pw, pp, ph, H, Ii, act, gp, gx.ptr, gw.ptr, ps, at.stream);
+        });
+        if (rc != UBEP_OK) return PyLong_FromLong(rc);
+        return Py_BuildValue("(NN)", gx.result(), gw.result());
+    } catch (...) {
+        return refused_or_raised();
+    }
+}
+
+// expert_linear(offset, count, status, x, w, bias, row_scale, residual, act, out, pre, stream): out, or the code
+PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        if (!want_args(n, 12)) return nullptr;
+        const RowsIn x(a[3], Py_None);
+        const Place at(x.t, a[11]);
+        const ubep_expert_rows_t r = rows_arg(a, at, x.R, x.cap);
+        const at::Tensor& w = need(a[4], "w");
+        if (w.dim() != 3) throw Refused("w", "not [experts, out, in]");
+        const int64_t N = w.size(1);
+        hold(w, "w", at.dev, at::kBFloat16, {(int64_t)r.num_experts, N, x.width});
+        const void* bias = maybe(a[5], "bias", at.dev, at::kBFloat16, {(int64_t)r.num_experts, N});
+        const float* scale = static_cast<const float*>(maybe(a[6], "row_scale", at.dev, at::kFloat, {x.R, x.cap}));
+        const void* residual = maybe(a[7], "residual", at.dev, at::kBFloat16, {x.R, x.cap, N});
+        const int act = (int)number(a[8]);
+        Output out(a[9], "out", at, at::kBFloat16, {x.R, x.cap, N}, true);
+        void* pre = maybe(a[10], "pre", at.dev, at::kBFloat16, {x.R, x.cap, N});
+        const void *px = x.t.data_ptr(), *pw = w.data_ptr();
+        const int32_t K = narrow(x.width, "x"), Ni = narrow(N, "w");
+        const int rc = without_gil([&] { return f_linear(&r, px, pw, bias, scale, residual, K, Ni, act, out.ptr, pre, at.stream); });
+        if (rc != UBEP_OK) return PyLong_FromLong(rc);
+        return out.result();
+    } catch (...) {
+        return refused_or_raised();
+    }
+}
+
+// expert_linear_backward(offset, count, status, x, w, grad_y, pre, row_scale, act, grad_pre, grad_x, grad_w, grad_bias, grad_row_scale,
+// stream): (grad_x, grad_w, grad_bias, grad_row_scale), or the code
+PyObject* py_linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    try {
+        if (!want_args(n, 15)) return nullptr;
+        const RowsIn x(a[3], Py_None);
+        const Place at(x.t, a[14]);
+        const ubep_expert_rows_t r = rows_arg(a, at, x.R, x.cap);
+        const at::Tensor& w = need(a[4], "w");
+        if (w.dim() != 3) throw Refused("w", "not [experts, out, in]");
+        const int64_t N = w.size(1);
+        hold(w, "w", at.dev, at::kBFloat16, {(int64_t)r.num_experts, N, x.width});
+        const at::Tensor& gy = need(a[5], "grad_y");
+        hold(gy, "grad_y", at.dev, at::kBFloat16, {x.R, x.cap, N});
+        const void* pre = maybe(a[6], "pre", at.dev, at::kBFloat16, {x.R, x.cap, N});
+        const float* scale = static_cast<const float*>(maybe(a[7], "row_scale", at.dev, at::kFloat, {x.R, x.cap}));
+        const int act = (int)number(a[8]);
+        at::Tensor room;
+        void* gp = maybe(a[9], "grad_pre", at.dev, at::kBFloat16, {x.R, x.cap, N});
+        if (!gp && (act != UBEP_ACT_NONE || scale)) {
+            room = at.scratch({x.R, x.cap, N}, at::kBFloat16);
+            gp = room.data_ptr();
+        }
+        Output gx(a[10], "grad_x", at, at::kBFloat16, {x.R, x.cap, x.width}, true), gw(a[11], "grad_w", at, at::kBFloat16, w.sizes(), true),
+            gb(a[12], "grad_bias", at, at::kBFloat16, {(int64_t)r.num_experts, N}, false),
+            gs(a[13], "grad_row_scale", at, at::kFloat, {x.R, x.cap}, false);
+        const void *px = x.t.data_ptr(), *pw = w.data_ptr(), *py = gy.data_ptr();
+        const int32_t K = narrow(x.width, "x"), Ni = narrow(N, "w");
+        const int rc = without_gil([&] {
+            return f_linear_backward(&r, px, pw, pre, scale, py, K, Ni, act, gp, gx.ptr, gw.ptr, gb.ptr, static_cast<float*>(gs.ptr), at.stream);
+        });
+        if (rc != UBEP_OK) return PyLong_FromLong(rc);
+        return Py_BuildValue("(NNNN)", gx.result(), gw.result(), gb.result(), gs.result());
+    } catch (...) {
+        return refused_or_raised();
+    }
+}
+
 // current_stream(): the handle of torch's current stream
 PyObject* py_current_stream(PyObject*, PyObject*) {
     try {
@@ -271,18 +609,19 @@ PyObject* py_current_stream(PyObject*, PyObject*) {
     }
 }
 
-// bind(dispatch, combine, get_dispatch_layout, dispatch_sync): addresses of the library's entry points
+// bind(dispatch, combine, get_dispatch_layout, dispatch_sync, route, route_backward, expert_gated, expert_gated_backward, expert_linear,
+// expert_linear_backward): addresses of the library's entry points
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!want_args(n, 4)) return nullptr;
-    void* p[4];
-    for (int i = 0; i < 4; ++i) {
-        p[i] = PyLong_AsVoidPtr(a[i]);
+    void** const to[] = {reinterpret_cast<void**>(&f_dispatch),       reinterpret_cast<void**>(&f_combine),
+                         reinterpret_cast<void**>(&f_layout),         reinterpret_cast<void**>(&f_dispatch_sync),
+                         reinterpret_cast<void**>(&f_route),          reinterpret_cast<void**>(&f_route_backward),
+                         reinterpret_cast<void**>(&f_gated),          reinterpret_cast<void**>(&f_gated_backward),
+                         reinterpret_cast<void**>(&f_linear),         reinterpret_cast<void**>(&f_linear_backward)};
+    if (!want_args(n, 10)) return nullptr;
+    for (int i = 0; i < 10; ++i) {
+        *to[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
-    f_dispatch = reinterpret_cast<decltype(f_dispatch)>(p[0]);
-    f_combine = reinterpret_cast<decltype(f_combine)>(p[1]);
-    f_layout = reinterpret_cast<decltype(f_layout)>(p[2]);
-    f_dispatch_sync = reinterpret_cast<decltype(f_dispatch_sync)>(p[3]);
     Py_RETURN_NONE;
 }
 
@@ -294,6 +633,12 @@ PyMethodDef kMethods[] = {
     UBEP_FAST("combine_new", py_combine_new),
     UBEP_FAST("layout", py_layout),
     UBEP_FAST("layout_new", py_layout_new),
+    UBEP_FAST("route", py_route),
+    UBEP_FAST("route_backward", py_route_backward),
+    UBEP_FAST("expert_gated", py_gated),
+    UBEP_FAST("expert_gated_backward", py_gated_backward),
+    UBEP_FAST("expert_linear", py_linear),
+    UBEP_FAST("expert_linear_backward", py_linear_backward),
     UBEP_FAST("bind", py_bind),
     {"current_stream", py_current_stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
