@@ -30,7 +30,8 @@ namespace {
 
 enum { kGated = 0, kLinear = 1, kRowsGrad = 2, kWeightsGrad = 3 };
 
-constexpr int kGemmThreads = 320;        // a loading warp, a multiplying warp, eight warps for the results
+// a loading warp, a multiplying warp, eight warps for the results (weights' gradient in pairs: one that mends the last rows)
+constexpr int gemm_threads(int mode, int cg) { return mode == kWeightsGrad && cg == 2 ? 352 : 320; }
 constexpr int kResultWarps = 8;
 constexpr int kStepK = 64;               // of the contraction per stage: 128 bytes of bf16, the swizzle's width
 constexpr int kHalfBytes = 128 * 128;    // 128 features of one stage
@@ -54,14 +55,25 @@ struct Product {
 };
 
 struct Shared {
-    uint64_t full[kMaxRing], empty[kMaxRing], acc_full[2], acc_empty[2], drained;
+    uint64_t full[kMaxRing], empty[kMaxRing], mended[kMaxRing], acc_full[2], acc_empty[2], drained;
     uint32_t tmem;
     int abort;
 };
 
-// Waits of a whole warp; all lanes agree on the outcome.
+// Waits of a whole warp; all lanes agree on the outcome.  CG = 2: for what the other CTA of the pair may have done.
+template <int CG>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity, Shared* sh, int32_t* status) {
-    const bool ok = mbar_wait_idle(bar, parity, &sh->abort);
+    bool ok;
+    if constexpr (CG == 1) {
+        ok = mbar_wait_idle(bar, parity, &sh->abort);
+    } else {
+        ok = mbar_try_wait_pair(bar, parity, 1000u);
+        if (!ok) {
+            const unsigned long long t_end = global_ns() + kWaitLimitNs;
+            while (!(ok = mbar_try_wait_pair(bar, parity, 1000u)))
+                if (*(volatile int*)&sh->abort || global_ns() > t_end) break;
+        }
+    }
     if (__all_sync(0xffffffffu, ok)) return true;
     if ((threadIdx.x & 31) == 0) {
         *(volatile int*)&sh->abort = 1;
@@ -80,7 +92,7 @@ struct Walk {
     TileWalk w;
     const Product& p;
     int per_row_tile, fb_tiles;
-    static constexpr int kFeatures = (MODE == kGated ? 128 : 256) * CG;
+    static constexpr int kFeatures = MODE == kGated ? 128 : 256;
     static constexpr bool kEvery = MODE == kWeightsGrad;
     static constexpr int kUnit = 16 * CG;
     __device__ __forceinline__ explicit Walk(const Product& p_) : p(p_) {
@@ -112,25 +124,42 @@ struct Walk {
     }
 };
 
+// Rows left .. of a stage of the weights' gradient, up to the next multiple of 16: behind the segment there is another expert's
+// row, or nobody's, and whatever it holds must not be multiplied.  Blocks of 64 rows x 128 bytes.
+__device__ __forceinline__ void clear_rows(uint8_t* stage, int blocks, int left, int lane) {
+    const int end = (left + 15) / 16 * 16;
+    for (int r = left; r < end; ++r)
+        for (int v = lane; v < blocks * 8; v += 32)
+            *reinterpret_cast<uint4*>(stage + (v >> 3) * 8192 + r * 128 + (v & 7) * 16) = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
 __device__ __forceinline__ uint4 ld_vec(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
 template <int MODE, int CG>
-__global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
-                                                                const __grid_constant__ CUtensorMap map_b, const Product p) {
+__global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
+                                                                          const __grid_constant__ CUtensorMap map_b, const Product p) {
     extern __shared__ uint8_t dynamic[];
     __shared__ Shared sh;
+    constexpr int kHalves = CG == 1 ? 2 : 1;                              // tiles of 128 features that this CTA multiplies with one tile of rows
+    constexpr bool kAcross = MODE == kRowsGrad || MODE == kWeightsGrad;   // the features' operand
+    constexpr bool kMends = MODE == kWeightsGrad && CG == 2;
+    constexpr int kBoxRows = 32 / CG;
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
     float* stage_tiles = reinterpret_cast<float*>(ring + (size_t)p.stages * p.stage_bytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CG == 1 ? 0 : (int)pair_rank();
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) {
             mbar_init(&sh.full[i], 1);
             mbar_init(&sh.empty[i], 1);
+            mbar_init(&sh.mended[i], 2);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.acc_full[i], 1);
-            mbar_init(&sh.acc_empty[i], kResultWarps);
+            mbar_init(&sh.acc_empty[i], kResultWarps * CG);
         }
         mbar_init(&sh.drained, 1);
         sh.abort = 0;
@@ -141,18 +170,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
             map_prefetch(&map_a);
             map_prefetch(&map_b);
         }
+        __syncwarp();
         tmem_alloc<CG>(&sh.tmem, kColumns);
     }
     tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    if constexpr (CG == 1) __syncthreads();
+    else pair_sync();
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t*)&sh.tmem;
     griddep_wait();
-    const int unit = blockIdx.x, units = gridDim.x;
+    const int unit = blockIdx.x / CG, units = gridDim.x / CG;
     Walk<MODE, CG> walk(p);
     Tile t;
-    constexpr bool kAcross = MODE == kRowsGrad || MODE == kWeightsGrad;   // the features' operand
-    constexpr int kBoxRows = 32;
     if (warp == 0) {
         // ------------------------------------------------------------------ loads
         int s = 0, used = 0;
@@ -161,30 +191,37 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
         for (int id = unit; ok && walk.find(id, t); id += units) {
             const int K = MODE == kWeightsGrad ? t.rows : p.K;
             const int steps = (K + kStepK - 1) / kStepK;
-            const bool two = MODE == kGated || t.f0 + 128 < p.F;
-            const int boxes = MODE == kWeightsGrad ? 4 : (t.rows + kBoxRows - 1) / kBoxRows;
+            const bool two = kHalves == 2 && (MODE == kGated || t.f0 + 128 < p.F);
+            const int f0 = t.f0 + rank * (MODE == kGated ? 64 : 128), fb0 = t.fb0 + rank * 128;
+            // (in a pair each CTA brings one half of the rows, or of x's features)
+            const int mine = CG == 1 ? t.rows : (t.rows + 31) / 32 * 16, row0 = t.row + rank * mine;
+            const int boxes = MODE == kWeightsGrad ? 4 / CG : (mine + kBoxRows - 1) / kBoxRows;
             const unsigned bytes = (two ? 2 : 1) * kHalfBytes + boxes * (MODE == kWeightsGrad ? 8192 : kBoxRows * 128);
             for (int k = 0; k < steps; ++k) {
-                ok = warp_wait(&sh.empty[s], phase ^ 1, &sh, p.status);
+                ok = warp_wait<CG>(&sh.empty[s], phase ^ 1, &sh, p.status);
                 if (!ok) break;
                 if (elect_one()) {
-                    const uint32_t a = smem_u32(ring + (size_t)s * p.stage_bytes), b = a + 2 * kHalfBytes, bar = smem_u32(&sh.full[s]);
-                    mbar_arrive_expect_tx(&sh.full[s], bytes);
+                    const uint32_t a = smem_u32(ring + (size_t)s * p.stage_bytes), b = a + kHalves * kHalfBytes;
+                    const uint32_t bar = CG == 1 || kMends ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
+                    if (CG == 1 || kMends) mbar_arrive_expect_tx(&sh.full[s], bytes);
+                    else if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2 * bytes);
                     const int k0 = k * kStepK;
-                    if constexpr (MODE == kGated) {
-                        tile_load<CG>(a, &map_a, k0, t.f0, 2 * t.e, bar);
-                        tile_load<CG>(a + kHalfBytes, &map_a, k0, t.f0, 2 * t.e + 1, bar);
+                    if constexpr (MODE == kGated && CG == 1) {
+                        tile_load<CG>(a, &map_a, k0, f0, 2 * t.e, bar);
+                        tile_load<CG>(a + kHalfBytes, &map_a, k0, f0, 2 * t.e + 1, bar);
+                    } else if constexpr (MODE == kGated) {
+                        tile_load5_pair(a, &map_a, k0, 0, 0, f0 / 8, t.e, bar);
                     } else if constexpr (MODE == kLinear) {
-                        tile_load<CG>(a, &map_a, k0, t.f0, t.e, bar);
-                        if (two) tile_load<CG>(a + kHalfBytes, &map_a, k0, t.f0 + 128, t.e, bar);
+                        tile_load<CG>(a, &map_a, k0, f0, t.e, bar);
+                        if (two) tile_load<CG>(a + kHalfBytes, &map_a, k0, f0 + 128, t.e, bar);
                     } else {
                         const int y = MODE == kRowsGrad ? k0 : t.row + k0, z = MODE == kRowsGrad ? t.e : 0;
-                        for (int j = 0; j < (two ? 4 : 2); ++j) tile_load<CG>(a + j * 8192, &map_a, t.f0 + 64 * j, y, z, bar);
+                        for (int j = 0; j < (two ? 4 : 2); ++j) tile_load<CG>(a + j * 8192, &map_a, f0 + 64 * j, y, z, bar);
                     }
                     if constexpr (MODE == kWeightsGrad)
-                        for (int j = 0; j < 4; ++j) tile_load<CG>(b + j * 8192, &map_b, t.fb0 + 64 * j, t.row + k0, 0, bar);
+                        for (int j = 0; j < boxes; ++j) tile_load<CG>(b + j * 8192, &map_b, fb0 + 64 * j, t.row + k0, 0, bar);
                     else
-                        for (int j = 0; j < boxes; ++j) tile_load<CG>(b + j * kBoxRows * 128, &map_b, k0, t.row + j * kBoxRows, 0, bar);
+                        for (int j = 0; j < boxes; ++j) tile_load<CG>(b + j * kBoxRows * 128, &map_b, k0, row0 + j * kBoxRows, 0, bar);
                 }
                 __syncwarp();
                 ++used;
@@ -194,8 +231,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                 }
             }
         }
-        if (!ok) {
-            // nothing may still be on its way into this CTA's shared memory when it leaves: the last copy of every stage
+        if (CG == 2 && ok)   // the products' last arrivals come to this CTA's barriers: it may not leave before them
+            for (int i = 0; ok && i < p.stages && i < used; ++i) {
+                s = s ? s - 1 : p.stages - 1;
+                if (s == p.stages - 1) phase ^= 1;
+                ok = warp_wait<CG>(&sh.empty[s], phase, &sh, p.status);
+            }
+        else if (!ok && (CG == 1 || kMends || rank == 0)) {
+            // nothing may still be on its way into shared memory when the CTA leaves: the last copy of every stage
             for (int i = 0; i < p.stages && i < used; ++i) {
                 s = s ? s - 1 : p.stages - 1;
                 if (s == p.stages - 1) phase ^= 1;
@@ -207,36 +250,27 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
         int s = 0, acc = 0;
         unsigned phase = 0, acc_phase = 0;
         bool ok = true;
-        for (int id = unit; ok && walk.find(id, t); id += units) {
+        for (int id = unit; rank == 0 && ok && walk.find(id, t); id += units) {
             const int K = MODE == kWeightsGrad ? t.rows : p.K;
             const int steps = (K + kStepK - 1) / kStepK;
             if (steps == 0) continue;
-            const bool two = MODE == kGated || t.f0 + 128 < p.F;
-            const int n = MODE == kWeightsGrad ? 256 : (t.rows + 15) / 16 * 16;
-            const uint32_t idesc = instruction(128, n, kAcross, MODE == kWeightsGrad);
-            const uint32_t d = tmem + acc * 2 * p.most;
-            ok = warp_wait(&sh.acc_empty[acc], acc_phase ^ 1, &sh, p.status);
+            const bool two = kHalves == 2 && (MODE == kGated || t.f0 + 128 < p.F);
+            const int n = MODE == kWeightsGrad ? 256 : (t.rows + 16 * CG - 1) / (16 * CG) * (16 * CG);
+            const uint32_t idesc = instruction(128 * CG, n, kAcross, MODE == kWeightsGrad);
+            const uint32_t d = tmem + acc * kHalves * p.most;
+            ok = warp_wait<CG>(&sh.acc_empty[acc], acc_phase ^ 1, &sh, p.status);
             if (!ok) break;
             tc_fence_after();
             for (int k = 0; k < steps; ++k) {
-                ok = warp_wait(&sh.full[s], phase, &sh, p.status);
+                ok = warp_wait<CG>(kMends ? &sh.mended[s] : &sh.full[s], phase, &sh, p.status);
                 if (!ok) break;
                 uint8_t* stage = ring + (size_t)s * p.stage_bytes;
                 const int left = K - k * kStepK;
-                if constexpr (MODE == kWeightsGrad) {
-                    if (left < kStepK) {
-                        // rows behind the segment are another expert's, or nobody's: whatever they hold must not be multiplied
-                        const int end = (left + 15) / 16 * 16;
-                        for (int r = left; r < end; ++r)
-                            for (int v = lane; v < 64; v += 32)
-                                *reinterpret_cast<uint4*>(stage + (v >> 3) * 8192 + r * 128 + (v & 7) * 16) = make_uint4(0, 0, 0, 0);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                    }
-                }
+                if constexpr (MODE == kWeightsGrad && CG == 1)
+                    if (left < kStepK) clear_rows(stage, kHalves * 2 + 4, left, lane);
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t a = smem_u32(stage), b = a + 2 * kHalfBytes;
+                    const uint32_t a = smem_u32(stage), b = a + kHalves * kHalfBytes;
                     const int parts = left < kStepK ? (left + 15) / 16 : 4;
                     for (int j = 0; j < parts; ++j) {
                         const uint64_t da = kAcross ? operand(a + j * 2048, 8192, 1024) : operand(a + j * 32, 16, 1024);
@@ -263,7 +297,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
             __syncwarp();
             mbar_wait(&sh.drained, 0, nullptr);
         }
-    } else {
+    } else if (warp < 2 + kResultWarps) {
         // ------------------------------------------------------------------ results
         const int quarter = warp & 3, group = (warp - 2) >> 2;   // lanes of tensor memory this warp may read; which columns
         float* tile = stage_tiles + (warp - 2) * kStageFloats;
@@ -273,30 +307,31 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
         for (int id = unit; ok && walk.find(id, t); id += units) {
             const bool empty = MODE == kWeightsGrad && t.rows == 0;
             if (!empty) {
-                ok = warp_wait(&sh.acc_full[acc], acc_phase, &sh, p.status);
+                ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
                 if (!ok) break;
                 tc_fence_after();
             }
-            const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * 2 * p.most;
+            const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * kHalves * p.most;
             if constexpr (MODE == kGated) {
-                const int f = t.f0 + quarter * 32 + (lane & 3) * 8;
-                for (int c = group * 8; c < t.rows; c += 16) {
-                    float g[8], u[8];
-                    tmem_ld8x2(d + c, d + p.most + c, g, u);
+                // one CTA: gate and up of 32 features in two accumulators, eight rows at a time; a pair: of 16 features in one
+                // accumulator (eight lanes gate, eight lanes up, twice), sixteen rows at a time
+                constexpr int kRows = CG == 1 ? 8 : 16, kVecs = 32 / kRows;
+                const int f = t.f0 + rank * 64 + quarter * (kVecs * 8) + (lane & (kVecs - 1)) * 8, mine = lane / kVecs;
+                for (int c = group * kRows; c < t.rows; c += 2 * kRows) {
+                    float g[16], *u = g + 8;
+                    if constexpr (CG == 1) tmem_ld8x2(d + c, d + p.most + c, g, u);
+                    else tmem_ld16(d + c, g);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        tile[i * kStagePitch + lane] = g[i];
-                        tile[(8 + i) * kStagePitch + lane] = u[i];
-                    }
+                    for (int i = 0; i < 16; ++i) tile[i * kStagePitch + lane] = g[i];
                     __syncwarp();
-                    const float* at = tile + (lane >> 2) * kStagePitch + (lane & 3) * 8;
+                    const float* at = tile + mine * kStagePitch + (lane & (kVecs - 1)) * (CG == 1 ? 8 : 16);
 #pragma unroll
                     for (int i = 0; i < 8; i += 4) {
                         *reinterpret_cast<float4*>(g + i) = *reinterpret_cast<const float4*>(at + i);
-                        *reinterpret_cast<float4*>(u + i) = *reinterpret_cast<const float4*>(at + 8 * kStagePitch + i);
+                        *reinterpret_cast<float4*>(u + i) = *reinterpret_cast<const float4*>(at + (CG == 1 ? 8 * kStagePitch : 8) + i);
                     }
                     __syncwarp();
-                    const int r = c + (lane >> 2);
+                    const int r = c + mine;
                     if (r < t.rows && f < p.F) {
                         const int64_t row = t.row + r;
                         if (p.pre) {
@@ -309,8 +344,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                     }
                 }
             } else if constexpr (MODE == kWeightsGrad) {
-                for (int h = 0; h < 2; ++h) {
-                    const int f = t.f0 + h * 128 + quarter * 32 + lane;
+                for (int h = 0; h < kHalves; ++h) {
+                    const int f = t.f0 + (h + rank) * 128 + quarter * 32 + lane;
                     if (f - lane >= p.F) break;
                     uint16_t* out = p.out + ((int64_t)t.e * p.F + f) * p.FB + t.fb0;
                     const int cols = min(256, p.FB - t.fb0);
@@ -329,8 +364,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                     }
                 }
             } else {
-                for (int h = 0; h < 2; ++h) {
-                    const int f = t.f0 + h * 128 + quarter * 32 + (lane & 3) * 8;
+                for (int h = 0; h < kHalves; ++h) {
+                    const int f = t.f0 + (h + rank) * 128 + quarter * 32 + (lane & 3) * 8;
                     if (f - (lane & 3) * 8 >= p.F) break;
                     float bias[8];
 #pragma unroll
@@ -378,16 +413,39 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
             if (!empty) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
+                if (lane == 0) {
+                    if constexpr (CG == 1) mbar_arrive(&sh.acc_empty[acc]);
+                    else mbar_arrive_pair(first_of_pair(&sh.acc_empty[acc]));
+                }
                 if (++acc == p.accs) {
                     acc = 0;
                     acc_phase ^= 1;
                 }
             }
         }
+    } else if constexpr (kMends) {
+        // ------------------------------------------------------------------ each CTA's operands of the weights' gradient
+        int s = 0;
+        unsigned phase = 0;
+        bool ok = true;
+        for (int id = unit; ok && walk.find(id, t); id += units)
+            for (int k = 0; k * kStepK < t.rows; ++k) {
+                ok = warp_wait<CG>(&sh.full[s], phase, &sh, p.status);
+                if (!ok) break;
+                if (t.rows - k * kStepK < kStepK) clear_rows(ring + (size_t)s * p.stage_bytes, 4, t.rows - k * kStepK, lane);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_pair(first_of_pair(&sh.mended[s]));
+                if (++s == p.stages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
     }
     tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    if constexpr (CG == 1) __syncthreads();
+    else pair_sync();
     tc_fence_after();
     griddep_launch();
     if (warp == 1) tmem_free<CG>(tmem, kColumns);
@@ -556,6 +614,18 @@ EncodeFn encoder() {
     return reinterpret_cast<EncodeFn>(f);
 }
 
+// Weights of the gated block for pairs, [E, 2, I, H] with I in eights: the box is 64 features' halves, eight rows of the gate's
+// matrix and eight of the other's in turn, so that both products of a feature end up in the same warp's lanes.
+bool make_gated_map(CUtensorMap* map, const void* base, uint64_t H, uint64_t I, uint64_t E) {
+    const EncodeFn encode = encoder();
+    if (!encode) return false;
+    const cuuint64_t dims[5] = {H, 8, 2, I / 8, E}, strides[4] = {H * 2, I * H * 2, 8 * H * 2, 2 * I * H * 2};
+    const cuuint32_t box[5] = {64, 8, 2, 8, 1}, steps[5] = {1, 1, 1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // bf16 [planes, rows, cols], boxes of `box_rows` x 64, 128-byte swizzle; what lies outside reads as zero.
 bool make_map(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t planes, unsigned box_rows) {
     const EncodeFn encode = encoder();
@@ -587,13 +657,14 @@ cudaError_t device_facts(DeviceFacts* f) {
     return e;
 }
 
-template <int MODE>
+template <int MODE, int CG>
 cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, Product p, cudaStream_t st) {
     DeviceFacts dev;
     cudaError_t e = device_facts(&dev);
     if (e != cudaSuccess) return e;
-    p.stage_bytes = 2 * kHalfBytes + p.most * 128;
-    p.accs = 4 * p.most <= kColumns ? 2 : 1;
+    constexpr int kHalves = CG == 1 ? 2 : 1;
+    p.stage_bytes = kHalves * kHalfBytes + p.most / CG * 128;
+    p.accs = 2 * kHalves * p.most <= kColumns ? 2 : 1;
     const int tiles = kResultWarps * kStageFloats * 4;
     const int room = dev.smem - 1024 - (int)sizeof(Shared) - tiles;
     p.stages = room / p.stage_bytes;
@@ -601,17 +672,17 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, Product p
     if (p.stages < 2) return cudaErrorInvalidConfiguration;
     const int smem = p.stages * p.stage_bytes + tiles + 1024;
     static std::atomic<int> granted[kAttrDevices];
-    e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, 1>), smem, granted);
+    e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, CG>), smem, granted);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(expert_kernel<MODE, 1>, dev.sms, kGemmThreads, (size_t)smem, st, false, 1, a, b, p);
+    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE, CG), (size_t)smem, st, false, CG, a, b, p);
 }
 
-// Rows per tile: the segments of a call are not known to the host, their capacity is.  Small pieces leave room for more stages
-// and a second accumulator.
-int rows_per_tile(const ubep_expert_rows_t& r) {
-    const int64_t each = (int64_t)r.num_ranks * r.rows_per_rank_cap / r.num_experts;
-    return each <= 64 ? 64 : each <= 128 ? 128 : 256;
-}
+// The segments of a call are not known to the host, their capacity is.
+int64_t rows_each(const ubep_expert_rows_t& r) { return (int64_t)r.num_ranks * r.rows_per_rank_cap / r.num_experts; }
+// Pairs of CTAs where there are rows enough to multiply; single CTAs where the weights are most of the traffic.
+bool in_pairs(const ubep_expert_rows_t& r) { return rows_each(r) > 64; }
+// Rows per tile.  Small pieces leave room for more stages and a second accumulator.
+int rows_per_tile(const ubep_expert_rows_t& r) { return in_pairs(r) ? 256 : 64; }
 
 dim3 row_grid(const ubep_expert_rows_t& r, const DeviceFacts& dev) {
     const int per = (dev.sms * 16 + r.num_experts - 1) / r.num_experts;
@@ -649,8 +720,9 @@ cudaError_t rows_grad(const ubep_expert_rows_t& r, const void* dz, const void* w
     p.out = static_cast<uint16_t*>(grad_x);
     p.status = r.status;
     CUtensorMap a, b;
-    if (!make_map(&a, w, K, N, r.num_experts, 64) || !make_map(&b, dz, N, all_rows(r), 1, 32)) return cudaErrorInvalidValue;
-    return launch_product<kRowsGrad>(a, b, p, st);
+    const bool pairs = in_pairs(r);
+    if (!make_map(&a, w, K, N, r.num_experts, 64) || !make_map(&b, dz, N, all_rows(r), 1, pairs ? 16 : 32)) return cudaErrorInvalidValue;
+    return pairs ? launch_product<kRowsGrad, 2>(a, b, p, st) : launch_product<kRowsGrad, 1>(a, b, p, st);
 }
 
 // dw[e, n, k] = sum_row dz[row, n] x[row, k]
@@ -664,7 +736,7 @@ cudaError_t weights_grad(const ubep_expert_rows_t& r, const void* dz, const void
     p.status = r.status;
     CUtensorMap a, b;
     if (!make_map(&a, dz, N, all_rows(r), 1, 64) || !make_map(&b, x, K, all_rows(r), 1, 64)) return cudaErrorInvalidValue;
-    return launch_product<kWeightsGrad>(a, b, p, st);
+    return in_pairs(r) ? launch_product<kWeightsGrad, 2>(a, b, p, st) : launch_product<kWeightsGrad, 1>(a, b, p, st);
 }
 
 }  // namespace
@@ -684,8 +756,11 @@ cudaError_t launch_expert_gated(const ubep_expert_rows_t& r, const void* x, cons
     p.pre = static_cast<uint16_t*>(pre);
     p.status = r.status;
     CUtensorMap a, b;
-    if (!make_map(&a, w, H, I, 2 * (uint64_t)r.num_experts, 128) || !make_map(&b, rows, H, all_rows(r), 1, 32)) return cudaErrorInvalidValue;
-    e = launch_product<kGated>(a, b, p, st);
+    const bool pairs = in_pairs(r);
+    if (!(pairs ? make_gated_map(&a, w, H, I, r.num_experts) : make_map(&a, w, H, I, 2 * (uint64_t)r.num_experts, 128)) ||
+        !make_map(&b, rows, H, all_rows(r), 1, pairs ? 16 : 32))
+        return cudaErrorInvalidValue;
+    e = pairs ? launch_product<kGated, 2>(a, b, p, st) : launch_product<kGated, 1>(a, b, p, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -732,8 +807,9 @@ cudaError_t launch_expert_linear(const ubep_expert_rows_t& r, const void* x, con
     p.row_scale = row_scale;
     p.status = r.status;
     CUtensorMap a, b;
-    if (!make_map(&a, w, K, N, r.num_experts, 128) || !make_map(&b, x, K, all_rows(r), 1, 32)) return cudaErrorInvalidValue;
-    const cudaError_t e = launch_product<kLinear>(a, b, p, st);
+    const bool pairs = in_pairs(r);
+    if (!make_map(&a, w, K, N, r.num_experts, 128) || !make_map(&b, x, K, all_rows(r), 1, pairs ? 16 : 32)) return cudaErrorInvalidValue;
+    const cudaError_t e = pairs ? launch_product<kLinear, 2>(a, b, p, st) : launch_product<kLinear, 1>(a, b, p, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

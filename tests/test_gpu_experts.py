@@ -29,6 +29,9 @@ SEGMENTS = {
     "gaps_out_of_order": (2, 300, [(200, 57), (10, 100), (0, 31), (250, 50)]),
     # what passes the region's end is left out, and an offset or a count that makes no sense has no rows
     "over_the_end": (2, 96, [(0, 60), (60, 100), (2 ** 31 - 1, 5), (96, 1), (-7, 20), (40, -3), (90, 2 ** 31 - 1), (50, 9)]),
+    "few_rows_in_long_regions": (1, 400, [(0, 1), (1, 0), (1, 16), (17, 31)]),
+    "long_over_the_end": (2, 500, [(0, 257), (257, 1000), (2 ** 31 - 1, 5), (-7, 400), (400, 33), (499, 2)]),
+    "two_pieces": (1, 3000, [(1, 255), (256, 256), (512, 513), (1025, 1290)]),
     "many_experts": (5, 40, [(i % 8 * 5, (i * 7) % 6) for i in range(40)]),
 }
 
