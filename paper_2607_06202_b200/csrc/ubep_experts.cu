@@ -36,8 +36,13 @@ constexpr int kResultWarps = 8;
 constexpr int kStepK = 64;               // of the contraction per stage: 128 bytes of bf16, the swizzle's width
 constexpr int kHalfBytes = 128 * 128;    // 128 features of one stage
 constexpr int kMaxRing = 8;
-constexpr int kStagePitch = 36;          // floats per row of a warp's transposition tile: conflict-free both ways
-constexpr int kStageFloats = 16 * kStagePitch;
+// Finished results go through shared memory, so that whole lines are written.  Rows: tiles of 16 rows per column group, two of them
+// in turn, or one beside those of the saved products; weights' gradient: a tile of 32 x 64 per warp, one tensor copy each.
+constexpr int kWide = 272;               // bytes per row of 128 results (16 to spread the banks), 16 rows per tile, 8 of them
+constexpr int kNarrow = 160;             // ... of 64 (the gated block in pairs): two neighbouring rows in different banks
+constexpr int kGroupBytes = 2 * 16 * kWide;
+constexpr int kBlockBytes = 32 * 128;
+constexpr int out_bytes(int mode) { return mode == kWeightsGrad ? kResultWarps * kBlockBytes : 2 * kGroupBytes; }
 constexpr int kColumns = 512;            // tensor memory: all of it (one CTA per SM)
 
 struct Product {
@@ -135,12 +140,14 @@ __device__ __forceinline__ void clear_rows(uint8_t* stage, int blocks, int left,
     __syncwarp();
 }
 
+__device__ __forceinline__ void put_bf16(uint8_t* at, float v) { *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16_rn(v); }
 __device__ __forceinline__ uint4 ld_vec(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
 template <int MODE, int CG>
 __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
-                                                                          const __grid_constant__ CUtensorMap map_b, const Product p) {
+                                                                          const __grid_constant__ CUtensorMap map_b,
+                                                                          const __grid_constant__ CUtensorMap map_out, const Product p) {
     extern __shared__ uint8_t dynamic[];
     __shared__ Shared sh;
     constexpr int kHalves = CG == 1 ? 2 : 1;                              // tiles of 128 features that this CTA multiplies with one tile of rows
@@ -148,7 +155,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
     constexpr bool kMends = MODE == kWeightsGrad && CG == 2;
     constexpr int kBoxRows = 32 / CG;
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
-    float* stage_tiles = reinterpret_cast<float*>(ring + (size_t)p.stages * p.stage_bytes);
+    uint8_t* results = ring + (size_t)p.stages * p.stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 1 ? 0 : (int)pair_rank();
     if (threadIdx.x == 0) {
@@ -300,129 +307,174 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
     } else if (warp < 2 + kResultWarps) {
         // ------------------------------------------------------------------ results
         const int quarter = warp & 3, group = (warp - 2) >> 2;   // lanes of tensor memory this warp may read; which columns
-        float* tile = stage_tiles + (warp - 2) * kStageFloats;
-        int acc = 0;
+        uint8_t* tiles = results + (MODE == kWeightsGrad ? (warp - 2) * kBlockBytes : group * kGroupBytes);
+        int acc = 0, flip = 0;
         unsigned acc_phase = 0;
-        bool ok = true;
-        for (int id = unit; ok && walk.find(id, t); id += units) {
+        for (int id = unit; walk.find(id, t); id += units) {
             const bool empty = MODE == kWeightsGrad && t.rows == 0;
             if (!empty) {
-                ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
-                if (!ok) break;
+                const bool ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
+                // (warps that meet at barriers below leave together)
+                if (MODE == kWeightsGrad ? !ok : group_or(1 + group, 128, !ok)) break;
                 tc_fence_after();
             }
             const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * kHalves * p.most;
-            if constexpr (MODE == kGated) {
-                // one CTA: gate and up of 32 features in two accumulators, eight rows at a time; a pair: of 16 features in one
-                // accumulator (eight lanes gate, eight lanes up, twice), sixteen rows at a time
-                constexpr int kRows = CG == 1 ? 8 : 16, kVecs = 32 / kRows;
-                const int f = t.f0 + rank * 64 + quarter * (kVecs * 8) + (lane & (kVecs - 1)) * 8, mine = lane / kVecs;
-                for (int c = group * kRows; c < t.rows; c += 2 * kRows) {
-                    float g[16], *u = g + 8;
-                    if constexpr (CG == 1) tmem_ld8x2(d + c, d + p.most + c, g, u);
-                    else tmem_ld16(d + c, g);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) tile[i * kStagePitch + lane] = g[i];
-                    __syncwarp();
-                    const float* at = tile + mine * kStagePitch + (lane & (kVecs - 1)) * (CG == 1 ? 8 : 16);
-#pragma unroll
-                    for (int i = 0; i < 8; i += 4) {
-                        *reinterpret_cast<float4*>(g + i) = *reinterpret_cast<const float4*>(at + i);
-                        *reinterpret_cast<float4*>(u + i) = *reinterpret_cast<const float4*>(at + (CG == 1 ? 8 * kStagePitch : 8) + i);
-                    }
-                    __syncwarp();
-                    const int r = c + mine;
-                    if (r < t.rows && f < p.F) {
-                        const int64_t row = t.row + r;
-                        if (p.pre) {
-                            st_vec(p.pre + row * 2 * p.F + f, pack8(g));
-                            st_vec(p.pre + (row * 2 + 1) * p.F + f, pack8(u));
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) g[i] = act_value(g[i], p.act) * u[i];
-                        st_vec(p.out + row * p.F + f, pack8(g));
-                    }
-                }
-            } else if constexpr (MODE == kWeightsGrad) {
-                for (int h = 0; h < kHalves; ++h) {
-                    const int f = t.f0 + (h + rank) * 128 + quarter * 32 + lane;
-                    if (f - lane >= p.F) break;
-                    uint16_t* out = p.out + ((int64_t)t.e * p.F + f) * p.FB + t.fb0;
-                    const int cols = min(256, p.FB - t.fb0);
-                    for (int c = group * 16; c < cols; c += 32) {
-                        float v[16];
-                        if (empty) {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-                        } else {
-                            tmem_ld16(d + h * p.most + c, v);
-                        }
-                        if (f < p.F) {
-                            st_vec(out + c, pack8(v));
-                            if (c + 8 < cols) st_vec(out + c + 8, pack8(v + 8));
-                        }
-                    }
-                }
-            } else {
-                for (int h = 0; h < kHalves; ++h) {
-                    const int f = t.f0 + (h + rank) * 128 + quarter * 32 + (lane & 3) * 8;
-                    if (f - (lane & 3) * 8 >= p.F) break;
-                    float bias[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
-                    if (p.bias && f < p.F) unpack8(ld_vec(p.bias + (int64_t)t.e * p.F + f), bias);
-                    for (int c = group * 16; c < t.rows; c += 32) {
-                        float v[16];
-                        tmem_ld16(d + h * p.most + c, v);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) tile[i * kStagePitch + lane] = v[i];
-                        __syncwarp();
-                        const float* at = tile + (lane >> 2) * kStagePitch + (lane & 3) * 8;
-#pragma unroll
-                        for (int i = 0; i < 16; i += 4)
-                            *reinterpret_cast<float4*>(v + i) = *reinterpret_cast<const float4*>(at + (i >> 3) * 8 * kStagePitch + (i & 7));
-                        __syncwarp();
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const int r = c + half * 8 + (lane >> 2);
-                            if (r >= t.rows || f >= p.F) continue;
-                            const int64_t row = t.row + r, place = row * p.F + f;
-                            float z[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) z[i] = v[half * 8 + i] + bias[i];
-                            if (p.pre) st_vec(p.pre + place, pack8(z));
-                            if (p.act)
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) z[i] = act_value(z[i], p.act);
-                            if (p.row_scale) {
-                                const float scale = ld_plain(p.row_scale + row);
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) z[i] *= scale;
-                            }
-                            if (p.residual) {
-                                float add[8];
-                                unpack8(ld_vec(p.residual + place), add);
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) z[i] += add[i];
-                            }
-                            st_vec(p.out + place, pack8(z));
-                        }
-                    }
-                }
-            }
-            if (!empty) {
+            bool held = !empty;   // the accumulator is given back once its last columns have been read
+            auto give_back = [&](bool when) {
+                if (!held || !when) return;
+                held = false;
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
                     if constexpr (CG == 1) mbar_arrive(&sh.acc_empty[acc]);
                     else mbar_arrive_pair(first_of_pair(&sh.acc_empty[acc]));
                 }
-                if (++acc == p.accs) {
-                    acc = 0;
-                    acc_phase ^= 1;
+            };
+            if constexpr (MODE == kWeightsGrad) {
+                for (int h = 0; h < kHalves; ++h) {
+                    const int f = t.f0 + (h + rank) * 128 + quarter * 32;
+                    for (int c = group * 128; c < group * 128 + 128; c += 64) {
+                        if (f >= p.F || t.fb0 + c >= p.FB) break;
+                        if (lane == 0) bulk_wait_read<0>();
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float v[16];
+                            if (empty) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) v[j] = 0.0f;
+                            } else {
+                                tmem_ld16(d + h * p.most + c + i * 16, v);
+                            }
+                            // (16-byte pieces in the order of the 128-byte swizzle: conflict-free)
+                            *reinterpret_cast<uint4*>(tiles + lane * 128 + (((2 * i) ^ (lane & 7)) << 4)) = pack8(v);
+                            *reinterpret_cast<uint4*>(tiles + lane * 128 + (((2 * i + 1) ^ (lane & 7)) << 4)) = pack8(v + 8);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tile_store(&map_out, t.fb0 + c, f, t.e, smem_u32(tiles));
+                            bulk_commit();
+                        }
+                    }
+                }
+            } else {
+                // one CTA and the gated block: gate and up of a feature in the same lane, in two accumulators, eight rows at a time; a
+                // pair: eight lanes gate, the next eight lanes up of the same features, so that a lane finishes every second row
+                constexpr int kRows = MODE == kGated && CG == 1 ? 8 : 16;
+                constexpr int kWidth = MODE == kGated && CG == 2 ? 64 : 128, kPitch = kWidth == 64 ? kNarrow : kWide;
+                constexpr int kTile = kRows * kPitch, kVecs = kWidth / 8, kPasses = kRows * kVecs / 128;
+                const int me = threadIdx.x - 64 - group * 128;   // thread of the column group
+                for (int h = 0; h < (MODE == kGated ? 1 : kHalves); ++h) {
+                    const int f0 = t.f0 + (MODE == kGated ? rank * kWidth : (h + rank) * 128);
+                    if (f0 >= p.F) break;
+                    const int col = MODE == kGated && CG == 2 ? quarter * 16 + (lane >> 4) * 8 + (lane & 7) : quarter * 32 + lane;
+                    // whole rows' pieces, 16 bytes per thread: rows and features of this thread's vectors
+                    const int vec_f = f0 + me % kVecs * 8, vec_row = me / kVecs;
+                    const bool vec_in = vec_f < p.F;
+                    uint4 ahead[kPasses];
+                    auto fetch = [&](int c) {   // the residual's next rows
+#pragma unroll
+                        for (int i = 0; i < kPasses; ++i) {
+                            const int r = c + vec_row + i * (128 / kVecs);
+                            ahead[i] = vec_in && r < t.rows ? ld_vec(p.residual + (int64_t)(t.row + r) * p.F + vec_f) : make_uint4(0, 0, 0, 0);
+                        }
+                    };
+                    auto put_out = [&](uint16_t* to, int64_t pitch, const uint8_t* from, int c) {
+#pragma unroll
+                        for (int i = 0; i < kPasses; ++i) {
+                            const int r = vec_row + i * (128 / kVecs);
+                            if (vec_in && c + r < t.rows)
+                                st_vec(to + (t.row + c + r) * pitch + vec_f, *reinterpret_cast<const uint4*>(from + r * kPitch + me % kVecs * 16));
+                        }
+                    };
+                    float bias = 0.0f;
+                    if constexpr (MODE == kLinear) {
+                        if (p.bias && f0 + col < p.F)
+                            bias = __uint_as_float((uint32_t)ld_plain(p.bias + (int64_t)t.e * p.F + f0 + col) << 16);
+                        if (p.residual) fetch(group * kRows);
+                    }
+                    for (int c = group * kRows; c < t.rows; c += 2 * kRows) {
+                        const bool last = c + 2 * kRows >= t.rows && (MODE == kGated || h == kHalves - 1 || f0 + 128 >= p.F);
+                        uint8_t* tile = tiles + (p.pre ? 0 : flip * kTile);
+                        float v[16];
+                        if constexpr (MODE == kGated && CG == 1) tmem_ld8x2(d + c, d + p.most + c, v, v + 8);
+                        else tmem_ld16(d + h * p.most + c, v);
+                        give_back(last);
+                        if constexpr (MODE == kGated) {
+                            float g[8], u[8];
+                            const bool up = lane & 8;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                if constexpr (CG == 1) {
+                                    g[i] = v[i];
+                                    u[i] = v[8 + i];
+                                } else {
+                                    const float other = __shfl_xor_sync(0xffffffffu, up ? v[2 * i] : v[2 * i + 1], 8);
+                                    g[i] = up ? other : v[2 * i];
+                                    u[i] = up ? v[2 * i + 1] : other;
+                                }
+                            }
+                            uint8_t* at = tile + (CG == 1 ? 0 : up * kPitch) + col * 2;
+                            constexpr int kStep = (CG == 1 ? 1 : 2) * kPitch;
+                            if (p.pre) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    put_bf16(at + i * kStep + kTile, g[i]);
+                                    put_bf16(at + i * kStep + 2 * kTile, u[i]);
+                                }
+                            }
+                            act_values<8>(g, p.act);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) put_bf16(at + i * kStep, g[i] * u[i]);
+                        } else {
+                            uint8_t* at = tile + col * 2;
+                            if constexpr (MODE == kLinear) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) v[i] += bias;
+                                if (p.pre) {
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) put_bf16(at + i * kPitch + kTile, v[i]);
+                                }
+                                act_values<16>(v, p.act);
+                                if (p.row_scale) {
+                                    const float scale = lane < 16 && c + lane < t.rows ? ld_plain(p.row_scale + t.row + c + lane) : 0.0f;
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) v[i] *= __shfl_sync(0xffffffffu, scale, i);
+                                }
+                                if (p.residual) {
+                                    // through the tile, where every thread finds the values of its own feature
+#pragma unroll
+                                    for (int i = 0; i < kPasses; ++i)
+                                        *reinterpret_cast<uint4*>(tile + (vec_row + i * (128 / kVecs)) * kPitch + me % kVecs * 16) = ahead[i];
+                                    if (c + 2 * kRows < t.rows) fetch(c + 2 * kRows);
+                                    group_sync(1 + group, 128);
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i)
+                                        v[i] += __uint_as_float((uint32_t) * reinterpret_cast<const uint16_t*>(at + i * kPitch) << 16);
+                                }
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) put_bf16(at + i * kPitch, v[i]);
+                        }
+                        group_sync(1 + group, 128);
+                        put_out(p.out, p.F, tile, c);
+                        if (p.pre) {
+                            put_out(p.pre, MODE == kGated ? 2 * p.F : p.F, tile + kTile, c);
+                            if (MODE == kGated) put_out(p.pre + p.F, 2 * p.F, tile + 2 * kTile, c);
+                            group_sync(1 + group, 128);
+                        }
+                        flip ^= 1;   // (the other tile's readers have met at a barrier since)
+                    }
                 }
             }
+            give_back(true);
+            if (!empty && ++acc == p.accs) {
+                acc = 0;
+                acc_phase ^= 1;
+            }
         }
+        if constexpr (MODE == kWeightsGrad) bulk_wait_all<0>();
     } else if constexpr (kMends) {
         // ------------------------------------------------------------------ each CTA's operands of the weights' gradient
         int s = 0;
@@ -658,14 +710,14 @@ cudaError_t device_facts(DeviceFacts* f) {
 }
 
 template <int MODE, int CG>
-cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, Product p, cudaStream_t st) {
+cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, Product p, cudaStream_t st) {
     DeviceFacts dev;
     cudaError_t e = device_facts(&dev);
     if (e != cudaSuccess) return e;
     constexpr int kHalves = CG == 1 ? 2 : 1;
     p.stage_bytes = kHalves * kHalfBytes + p.most / CG * 128;
     p.accs = 2 * kHalves * p.most <= kColumns ? 2 : 1;
-    const int tiles = kResultWarps * kStageFloats * 4;
+    const int tiles = out_bytes(MODE);
     const int room = dev.smem - 1024 - (int)sizeof(Shared) - tiles;
     p.stages = room / p.stage_bytes;
     if (p.stages > kMaxRing) p.stages = kMaxRing;
@@ -674,7 +726,7 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, Product p
     static std::atomic<int> granted[kAttrDevices];
     e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, CG>), smem, granted);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE, CG), (size_t)smem, st, false, CG, a, b, p);
+    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE, CG), (size_t)smem, st, false, CG, a, b, out, p);
 }
 
 // The segments of a call are not known to the host, their capacity is.
@@ -722,7 +774,7 @@ cudaError_t rows_grad(const ubep_expert_rows_t& r, const void* dz, const void* w
     CUtensorMap a, b;
     const bool pairs = in_pairs(r);
     if (!make_map(&a, w, K, N, r.num_experts, 64) || !make_map(&b, dz, N, all_rows(r), 1, pairs ? 16 : 32)) return cudaErrorInvalidValue;
-    return pairs ? launch_product<kRowsGrad, 2>(a, b, p, st) : launch_product<kRowsGrad, 1>(a, b, p, st);
+    return pairs ? launch_product<kRowsGrad, 2>(a, b, b, p, st) : launch_product<kRowsGrad, 1>(a, b, b, p, st);
 }
 
 // dw[e, n, k] = sum_row dz[row, n] x[row, k]
@@ -734,9 +786,10 @@ cudaError_t weights_grad(const ubep_expert_rows_t& r, const void* dz, const void
     p.most = 256;
     p.out = static_cast<uint16_t*>(grad_w);
     p.status = r.status;
-    CUtensorMap a, b;
-    if (!make_map(&a, dz, N, all_rows(r), 1, 64) || !make_map(&b, x, K, all_rows(r), 1, 64)) return cudaErrorInvalidValue;
-    return in_pairs(r) ? launch_product<kWeightsGrad, 2>(a, b, p, st) : launch_product<kWeightsGrad, 1>(a, b, p, st);
+    CUtensorMap a, b, out;
+    if (!make_map(&a, dz, N, all_rows(r), 1, 64) || !make_map(&b, x, K, all_rows(r), 1, 64) || !make_map(&out, grad_w, K, N, r.num_experts, 32))
+        return cudaErrorInvalidValue;
+    return in_pairs(r) ? launch_product<kWeightsGrad, 2>(a, b, out, p, st) : launch_product<kWeightsGrad, 1>(a, b, out, p, st);
 }
 
 }  // namespace
@@ -760,7 +813,7 @@ cudaError_t launch_expert_gated(const ubep_expert_rows_t& r, const void* x, cons
     if (!(pairs ? make_gated_map(&a, w, H, I, r.num_experts) : make_map(&a, w, H, I, 2 * (uint64_t)r.num_experts, 128)) ||
         !make_map(&b, rows, H, all_rows(r), 1, pairs ? 16 : 32))
         return cudaErrorInvalidValue;
-    e = pairs ? launch_product<kGated, 2>(a, b, p, st) : launch_product<kGated, 1>(a, b, p, st);
+    e = pairs ? launch_product<kGated, 2>(a, b, b, p, st) : launch_product<kGated, 1>(a, b, b, p, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -809,7 +862,7 @@ cudaError_t launch_expert_linear(const ubep_expert_rows_t& r, const void* x, con
     CUtensorMap a, b;
     const bool pairs = in_pairs(r);
     if (!make_map(&a, w, K, N, r.num_experts, 128) || !make_map(&b, x, K, all_rows(r), 1, pairs ? 16 : 32)) return cudaErrorInvalidValue;
-    const cudaError_t e = pairs ? launch_product<kLinear, 2>(a, b, p, st) : launch_product<kLinear, 1>(a, b, p, st);
+    const cudaError_t e = pairs ? launch_product<kLinear, 2>(a, b, b, p, st) : launch_product<kLinear, 1>(a, b, b, p, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

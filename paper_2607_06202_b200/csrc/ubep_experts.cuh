@@ -15,6 +15,20 @@ __device__ __forceinline__ float act_value(float z, int act) {
     if (act == kActRelu) return z > 0.0f || z != z ? z : 0.0f;
     return z;
 }
+// The same of several at once: one branch for all of them, so that they are worked on side by side.
+template <int N>
+__device__ __forceinline__ void act_values(float* z, int act) {
+    if (act == kActSilu) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = act_value(z[i], kActSilu);
+    } else if (act == kActGelu) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = act_value(z[i], kActGelu);
+    } else if (act == kActRelu) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = act_value(z[i], kActRelu);
+    }
+}
 // The value and the derivative.
 __device__ __forceinline__ void act_both(float z, int act, float& value, float& slope) {
     if (act == kActSilu) {
