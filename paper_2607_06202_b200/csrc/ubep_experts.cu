@@ -60,7 +60,7 @@ struct Product {
 };
 
 struct Shared {
-    uint64_t full[kMaxRing], empty[kMaxRing], mended[kMaxRing], acc_full[2], acc_empty[2], drained;
+    uint64_t full[kMaxRing], empty[kMaxRing], ends[kMaxRing], cleared[kMaxRing], acc_full[2], acc_empty[2], drained;
     uint32_t tmem;
     int abort;
 };
@@ -132,7 +132,7 @@ struct Walk {
 // Rows left .. of a stage of the weights' gradient, up to the next multiple of 16: behind the segment there is another expert's
 // row, or nobody's, and whatever it holds must not be multiplied.  Blocks of 64 rows x 128 bytes.
 __device__ __forceinline__ void clear_rows(uint8_t* stage, int blocks, int left, int lane) {
-    const int end = (left + 15) / 16 * 16;
+    const int end = (left + 15) / 16 * 16;   // (the instructions take 16 rows each)
     for (int r = left; r < end; ++r)
         for (int v = lane; v < blocks * 8; v += 32)
             *reinterpret_cast<uint4*>(stage + (v >> 3) * 8192 + r * 128 + (v & 7) * 16) = make_uint4(0, 0, 0, 0);
@@ -147,13 +147,12 @@ __device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast
 template <int MODE, int CG>
 __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                           const __grid_constant__ CUtensorMap map_b,
-                                                                          const __grid_constant__ CUtensorMap map_out, const Product p) {
+                                                                          const __grid_constant__ CUtensorMap map_c, const Product p) {
     extern __shared__ uint8_t dynamic[];
     __shared__ Shared sh;
     constexpr int kHalves = CG == 1 ? 2 : 1;                              // tiles of 128 features that this CTA multiplies with one tile of rows
     constexpr bool kAcross = MODE == kRowsGrad || MODE == kWeightsGrad;   // the features' operand
     constexpr bool kMends = MODE == kWeightsGrad && CG == 2;
-    constexpr int kBoxRows = 32 / CG;
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
     uint8_t* results = ring + (size_t)p.stages * p.stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -162,7 +161,10 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
         for (int i = 0; i < p.stages; ++i) {
             mbar_init(&sh.full[i], 1);
             mbar_init(&sh.empty[i], 1);
-            mbar_init(&sh.mended[i], 2);
+        }
+        for (int i = 0; i < kMaxRing; ++i) {
+            mbar_init(&sh.ends[i], 1);
+            mbar_init(&sh.cleared[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.acc_full[i], 1);
@@ -176,6 +178,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
         if (lane == 0) {
             map_prefetch(&map_a);
             map_prefetch(&map_b);
+            map_prefetch(&map_c);
         }
         __syncwarp();
         tmem_alloc<CG>(&sh.tmem, kColumns);
@@ -192,7 +195,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
     Tile t;
     if (warp == 0) {
         // ------------------------------------------------------------------ loads
-        int s = 0, used = 0;
+        int s = 0, used = 0, ends = 0;
         unsigned phase = 0;
         bool ok = true;
         for (int id = unit; ok && walk.find(id, t); id += units) {
@@ -202,17 +205,23 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
             const int f0 = t.f0 + rank * (MODE == kGated ? 64 : 128), fb0 = t.fb0 + rank * 128;
             // (in a pair each CTA brings one half of the rows, or of x's features)
             const int mine = CG == 1 ? t.rows : (t.rows + 31) / 32 * 16, row0 = t.row + rank * mine;
-            const int boxes = MODE == kWeightsGrad ? 4 / CG : (mine + kBoxRows - 1) / kBoxRows;
-            const unsigned bytes = (two ? 2 : 1) * kHalfBytes + boxes * (MODE == kWeightsGrad ? 8192 : kBoxRows * 128);
+            // (boxes of 64 and of 16 rows: a copy costs the loading warp some 55 cycles, eight copies of 16 rows nearly the whole step)
+            const int small = MODE == kWeightsGrad ? 0 : (mine + 15) / 16 % 4, large = MODE == kWeightsGrad ? 4 / CG : (mine + 15) / 64;
+            const unsigned bytes = (two ? 2 : 1) * kHalfBytes + large * 8192 + small * 2048;
             for (int k = 0; k < steps; ++k) {
                 ok = warp_wait<CG>(&sh.empty[s], phase ^ 1, &sh, p.status);
                 if (!ok) break;
                 if (elect_one()) {
                     const uint32_t a = smem_u32(ring + (size_t)s * p.stage_bytes), b = a + kHalves * kHalfBytes;
-                    const uint32_t bar = CG == 1 || kMends ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
-                    if (CG == 1 || kMends) mbar_arrive_expect_tx(&sh.full[s], bytes);
-                    else if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2 * bytes);
                     const int k0 = k * kStepK;
+                    uint32_t bar = CG == 1 ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
+                    if (kMends && K - k0 < kStepK) {   // each CTA counts its own last rows, which have to be mended
+                        uint64_t* end = &sh.ends[ends % kMaxRing];
+                        bar = smem_u32(end);
+                        mbar_arrive_expect_tx(end, bytes);
+                    } else if (rank == 0) {
+                        mbar_arrive_expect_tx(&sh.full[s], CG * bytes);
+                    }
                     if constexpr (MODE == kGated && CG == 1) {
                         tile_load<CG>(a, &map_a, k0, f0, 2 * t.e, bar);
                         tile_load<CG>(a + kHalfBytes, &map_a, k0, f0, 2 * t.e + 1, bar);
@@ -226,11 +235,15 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
                         for (int j = 0; j < (two ? 4 : 2); ++j) tile_load<CG>(a + j * 8192, &map_a, f0 + 64 * j, y, z, bar);
                     }
                     if constexpr (MODE == kWeightsGrad)
-                        for (int j = 0; j < boxes; ++j) tile_load<CG>(b + j * 8192, &map_b, fb0 + 64 * j, t.row + k0, 0, bar);
-                    else
-                        for (int j = 0; j < boxes; ++j) tile_load<CG>(b + j * kBoxRows * 128, &map_b, k0, row0 + j * kBoxRows, 0, bar);
+                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, fb0 + 64 * j, t.row + k0, 0, bar);
+                    else {
+                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, k0, row0 + j * 64, 0, bar);
+                        for (int j = 0; j < small; ++j)
+                            tile_load<CG>(b + large * 8192 + j * 2048, &map_c, k0, row0 + large * 64 + j * 16, 0, bar);
+                    }
                 }
                 __syncwarp();
+                ends += kMends && K - k * kStepK < kStepK;
                 ++used;
                 if (++s == p.stages) {
                     s = 0;
@@ -244,9 +257,10 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
                 if (s == p.stages - 1) phase ^= 1;
                 ok = warp_wait<CG>(&sh.empty[s], phase, &sh, p.status);
             }
-        else if (!ok && (CG == 1 || kMends || rank == 0)) {
-            // nothing may still be on its way into shared memory when the CTA leaves: the last copy of every stage
-            for (int i = 0; i < p.stages && i < used; ++i) {
+        else if (!ok) {
+            // nothing may still be on its way into shared memory when the CTA leaves: the last copy of every stage (a pair leaves
+            // together, and the first CTA's barriers count for both)
+            for (int i = 0; rank == 0 && i < p.stages && i < used; ++i) {
                 s = s ? s - 1 : p.stages - 1;
                 if (s == p.stages - 1) phase ^= 1;
                 mbar_wait(&sh.full[s], phase, nullptr);
@@ -269,7 +283,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
             if (!ok) break;
             tc_fence_after();
             for (int k = 0; k < steps; ++k) {
-                ok = warp_wait<CG>(kMends ? &sh.mended[s] : &sh.full[s], phase, &sh, p.status);
+                ok = warp_wait<CG>(&sh.full[s], phase, &sh, p.status);
                 if (!ok) break;
                 uint8_t* stage = ring + (size_t)s * p.stage_bytes;
                 const int left = K - k * kStepK;
@@ -353,7 +367,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            tile_store(&map_out, t.fb0 + c, f, t.e, smem_u32(tiles));
+                            tile_store(&map_c, t.fb0 + c, f, t.e, smem_u32(tiles));
                             bulk_commit();
                         }
                     }
@@ -476,23 +490,30 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
         }
         if constexpr (MODE == kWeightsGrad) bulk_wait_all<0>();
     } else if constexpr (kMends) {
-        // ------------------------------------------------------------------ each CTA's operands of the weights' gradient
-        int s = 0;
-        unsigned phase = 0;
+        // ------------------------------------------------------------------ last rows of a segment in the weights' gradient
+        // Both CTAs clear what is behind them in their own operands; the second tells the first, and the first completes the stage
+        // that its products wait for.  (Done for every step, the arrival at the other CTA alone took more than twice a step's time.)
+        int s = 0, ends = 0;
         bool ok = true;
-        for (int id = unit; ok && walk.find(id, t); id += units)
-            for (int k = 0; k * kStepK < t.rows; ++k) {
-                ok = warp_wait<CG>(&sh.full[s], phase, &sh, p.status);
+        for (int id = unit; ok && walk.find(id, t); id += units) {
+            s += (t.rows + kStepK - 1) / kStepK;
+            const int left = t.rows % kStepK;
+            if (!left) continue;
+            const int at = (s - 1) % p.stages, end = ends % kMaxRing;
+            const unsigned phase = ends / kMaxRing & 1;
+            ok = warp_wait<CG>(&sh.ends[end], phase, &sh, p.status);
+            if (!ok) break;
+            clear_rows(ring + (size_t)at * p.stage_bytes, 4, left, lane);
+            if (rank == 0) {
+                ok = warp_wait<CG>(&sh.cleared[end], phase, &sh, p.status);
                 if (!ok) break;
-                if (t.rows - k * kStepK < kStepK) clear_rows(ring + (size_t)s * p.stage_bytes, 4, t.rows - k * kStepK, lane);
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_pair(first_of_pair(&sh.mended[s]));
-                if (++s == p.stages) {
-                    s = 0;
-                    phase ^= 1;
-                }
+                if (lane == 0) mbar_arrive(&sh.full[at]);
+            } else if (lane == 0) {
+                mbar_arrive_pair(first_of_pair(&sh.cleared[end]));
             }
+            ++ends;
+            s %= p.stages;
+        }
     }
     tc_fence_before();
     __syncwarp();
@@ -710,7 +731,7 @@ cudaError_t device_facts(DeviceFacts* f) {
 }
 
 template <int MODE, int CG>
-cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, Product p, cudaStream_t st) {
+cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, Product p, cudaStream_t st) {
     DeviceFacts dev;
     cudaError_t e = device_facts(&dev);
     if (e != cudaSuccess) return e;
@@ -726,7 +747,7 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     static std::atomic<int> granted[kAttrDevices];
     e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, CG>), smem, granted);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE, CG), (size_t)smem, st, false, CG, a, b, out, p);
+    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE, CG), (size_t)smem, st, false, CG, a, b, c, p);
 }
 
 // The segments of a call are not known to the host, their capacity is.
@@ -735,6 +756,12 @@ int64_t rows_each(const ubep_expert_rows_t& r) { return (int64_t)r.num_ranks * r
 bool in_pairs(const ubep_expert_rows_t& r) { return rows_each(r) > 64; }
 // Rows per tile.  Small pieces leave room for more stages and a second accumulator.
 int rows_per_tile(const ubep_expert_rows_t& r) { return in_pairs(r) ? 256 : 64; }
+
+uint64_t all_rows(const ubep_expert_rows_t& r) { return (uint64_t)r.num_ranks * r.rows_per_rank_cap; }
+// Rows of all regions, [R * cap, width], in boxes of 64 and of 16 rows.
+bool make_rows_maps(CUtensorMap* large, CUtensorMap* small, const void* rows, int width, const ubep_expert_rows_t& r) {
+    return make_map(large, rows, width, all_rows(r), 1, 64) && make_map(small, rows, width, all_rows(r), 1, 16);
+}
 
 dim3 row_grid(const ubep_expert_rows_t& r, const DeviceFacts& dev) {
     const int per = (dev.sms * 16 + r.num_experts - 1) / r.num_experts;
@@ -760,7 +787,6 @@ cudaError_t rows_in(const ubep_expert_rows_t& r, const void* x, const float* x_s
     return cudaGetLastError();
 }
 
-uint64_t all_rows(const ubep_expert_rows_t& r) { return (uint64_t)r.num_ranks * r.rows_per_rank_cap; }
 
 // dx[row, k] = sum_n dz[row, n] w[e, n, k]
 cudaError_t rows_grad(const ubep_expert_rows_t& r, const void* dz, const void* w, int K, int N, void* grad_x, cudaStream_t st) {
@@ -771,10 +797,10 @@ cudaError_t rows_grad(const ubep_expert_rows_t& r, const void* dz, const void* w
     p.most = rows_per_tile(r);
     p.out = static_cast<uint16_t*>(grad_x);
     p.status = r.status;
-    CUtensorMap a, b;
+    CUtensorMap a, b, c;
     const bool pairs = in_pairs(r);
-    if (!make_map(&a, w, K, N, r.num_experts, 64) || !make_map(&b, dz, N, all_rows(r), 1, pairs ? 16 : 32)) return cudaErrorInvalidValue;
-    return pairs ? launch_product<kRowsGrad, 2>(a, b, b, p, st) : launch_product<kRowsGrad, 1>(a, b, b, p, st);
+    if (!make_map(&a, w, K, N, r.num_experts, 64) || !make_rows_maps(&b, &c, dz, N, r)) return cudaErrorInvalidValue;
+    return pairs ? launch_product<kRowsGrad, 2>(a, b, c, p, st) : launch_product<kRowsGrad, 1>(a, b, c, p, st);
 }
 
 // dw[e, n, k] = sum_row dz[row, n] x[row, k]
@@ -808,12 +834,12 @@ cudaError_t launch_expert_gated(const ubep_expert_rows_t& r, const void* x, cons
     p.out = static_cast<uint16_t*>(h);
     p.pre = static_cast<uint16_t*>(pre);
     p.status = r.status;
-    CUtensorMap a, b;
+    CUtensorMap a, b, c;
     const bool pairs = in_pairs(r);
     if (!(pairs ? make_gated_map(&a, w, H, I, r.num_experts) : make_map(&a, w, H, I, 2 * (uint64_t)r.num_experts, 128)) ||
-        !make_map(&b, rows, H, all_rows(r), 1, pairs ? 16 : 32))
+        !make_rows_maps(&b, &c, rows, H, r))
         return cudaErrorInvalidValue;
-    e = pairs ? launch_product<kGated, 2>(a, b, b, p, st) : launch_product<kGated, 1>(a, b, b, p, st);
+    e = pairs ? launch_product<kGated, 2>(a, b, c, p, st) : launch_product<kGated, 1>(a, b, c, p, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -859,10 +885,10 @@ cudaError_t launch_expert_linear(const ubep_expert_rows_t& r, const void* x, con
     p.residual = static_cast<const uint16_t*>(residual);
     p.row_scale = row_scale;
     p.status = r.status;
-    CUtensorMap a, b;
+    CUtensorMap a, b, c;
     const bool pairs = in_pairs(r);
-    if (!make_map(&a, w, K, N, r.num_experts, 128) || !make_map(&b, x, K, all_rows(r), 1, pairs ? 16 : 32)) return cudaErrorInvalidValue;
-    const cudaError_t e = pairs ? launch_product<kLinear, 2>(a, b, b, p, st) : launch_product<kLinear, 1>(a, b, b, p, st);
+    if (!make_map(&a, w, K, N, r.num_experts, 128) || !make_rows_maps(&b, &c, x, K, r)) return cudaErrorInvalidValue;
+    const cudaError_t e = pairs ? launch_product<kLinear, 2>(a, b, c, p, st) : launch_product<kLinear, 1>(a, b, c, p, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
