@@ -486,7 +486,7 @@ enum { UBEP_ACT_NONE = 0, UBEP_ACT_SILU = 1, UBEP_ACT_GELU = 2 /* x Phi(x) */, U
  * Gated feed-forward block: h = act(x Wg_e^T) * (x Wu_e^T) for every row x of expert e.
  * x [dev]: bf16 [R, cap, H]; with x_scale [dev] fp32 [R, cap, H / 128], e4m3 [R, cap, H] with one
  * scale per 128 channels as an FP8 dispatch delivers them (H a multiple of 128), and scratch [dev]
- * bf16 [R, cap, H] for the rows as bf16.  w [dev] bf16 [E, 2, I, H]: the gate's matrix, then the other.
+ * bf16 [R, cap, H] for the values as bf16, which holds them exactly (the scales multiply the sums over their channels).  w [dev] bf16 [E, 2, I, H]: the gate's matrix, then the other.
  * h [dev] bf16 [R, cap, I].  pre [dev] bf16 [R, cap, 2, I] or NULL: both products, for
  * ubep_expert_gated_backward.  H and I multiples of 8.  One launch, two with FP8 rows.
  */
@@ -498,8 +498,8 @@ int ubep_expert_gated(const ubep_expert_rows_t *rows /*[host]*/, const void *x /
  * Its gradients: with dg = grad_h u act'(g) and du = grad_h act(g), g and u from pre,
  * grad_x = dg Wg + du Wu ([dev] bf16 [R, cap, H]) and grad_w = [dg^T x, du^T x] ([dev] bf16 [E, 2, I, H]; zero for an
  * expert without rows).  Either may be NULL.  grad_pre [dev] bf16 [R, cap, 2, I]: room for dg and du,
- * rounded to bf16 for the products; may be pre itself.  x, x_scale, scratch as above (scratch is needed for grad_w
- * alone).  Up to four launches.
+ * rounded to bf16 for the products; may be pre itself.  x, x_scale as above; with x_scale grad_w takes its rows as the sum of
+ * two bf16 numbers each, in scratch [dev] bf16 [2, R, cap, H].  Up to four launches.
  */
 int ubep_expert_gated_backward(const ubep_expert_rows_t *rows /*[host]*/, const void *x /*[dev]*/,
                                const float *x_scale /*[dev]*/, const void *w /*[dev]*/, const void *pre /*[dev]*/,

@@ -28,10 +28,12 @@ namespace ubep {
 
 namespace {
 
-enum { kGated = 0, kLinear = 1, kRowsGrad = 2, kWeightsGrad = 3 };
+enum { kGated = 0, kLinear = 1, kRowsGrad = 2, kWeightsGrad = 3, kGatedScaled = 4 };
+__host__ __device__ constexpr bool gated(int mode) { return mode == kGated || mode == kGatedScaled; }   // kGatedScaled: rows of an FP8 dispatch
 
-// a loading warp, a multiplying warp, eight warps for the results (weights' gradient in pairs: one that mends the last rows)
-constexpr int gemm_threads(int mode, int cg) { return mode == kWeightsGrad && cg == 2 ? 352 : 320; }
+// A warpgroup with a loading warp, a multiplying warp and (weights' gradient in pairs) one that mends the last rows; two for the results.
+constexpr int kGemmThreads = 384;
+constexpr int kFirstResult = 4;
 constexpr int kResultWarps = 8;
 constexpr int kStepK = 64;               // of the contraction per stage: 128 bytes of bf16, the swizzle's width
 constexpr int kHalfBytes = 128 * 128;    // 128 features of one stage
@@ -55,7 +57,8 @@ struct Product {
     int act;
     uint16_t *out, *pre;
     const uint16_t *bias, *residual;
-    const float* row_scale;
+    const float *row_scale, *x_scale;
+    int planes;      // weights' gradient: 2 = x is the sum of two bf16 arrays
     int32_t* status;
 };
 
@@ -97,7 +100,7 @@ struct Walk {
     TileWalk w;
     const Product& p;
     int per_row_tile, fb_tiles;
-    static constexpr int kFeatures = MODE == kGated ? 128 : 256;
+    static constexpr int kFeatures = gated(MODE) ? 128 : 256;
     static constexpr bool kEvery = MODE == kWeightsGrad;
     static constexpr int kUnit = 16 * CG;
     __device__ __forceinline__ explicit Walk(const Product& p_) : p(p_) {
@@ -145,7 +148,7 @@ __device__ __forceinline__ uint4 ld_vec(const uint16_t* p) { return *reinterpret
 __device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
 template <int MODE, int CG>
-__global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
+__global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                           const __grid_constant__ CUtensorMap map_b,
                                                                           const __grid_constant__ CUtensorMap map_c, const Product p) {
     extern __shared__ uint8_t dynamic[];
@@ -153,6 +156,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
     constexpr int kHalves = CG == 1 ? 2 : 1;                              // tiles of 128 features that this CTA multiplies with one tile of rows
     constexpr bool kAcross = MODE == kRowsGrad || MODE == kWeightsGrad;   // the features' operand
     constexpr bool kMends = MODE == kWeightsGrad && CG == 2;
+    constexpr bool kScaled = MODE == kGatedScaled;
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
     uint8_t* results = ring + (size_t)p.stages * p.stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -193,140 +197,87 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
     const int unit = blockIdx.x / CG, units = gridDim.x / CG;
     Walk<MODE, CG> walk(p);
     Tile t;
-    if (warp == 0) {
-        // ------------------------------------------------------------------ loads
-        int s = 0, used = 0, ends = 0;
-        unsigned phase = 0;
-        bool ok = true;
-        for (int id = unit; ok && walk.find(id, t); id += units) {
-            const int K = MODE == kWeightsGrad ? t.rows : p.K;
-            const int steps = (K + kStepK - 1) / kStepK;
-            const bool two = kHalves == 2 && (MODE == kGated || t.f0 + 128 < p.F);
-            const int f0 = t.f0 + rank * (MODE == kGated ? 64 : 128), fb0 = t.fb0 + rank * 128;
-            // (in a pair each CTA brings one half of the rows, or of x's features)
-            const int mine = CG == 1 ? t.rows : (t.rows + 31) / 32 * 16, row0 = t.row + rank * mine;
-            // (boxes of 64 and of 16 rows: a copy costs the loading warp some 55 cycles, eight copies of 16 rows nearly the whole step)
-            const int small = MODE == kWeightsGrad ? 0 : (mine + 15) / 16 % 4, large = MODE == kWeightsGrad ? 4 / CG : (mine + 15) / 64;
-            const unsigned bytes = (two ? 2 : 1) * kHalfBytes + large * 8192 + small * 2048;
-            for (int k = 0; k < steps; ++k) {
-                ok = warp_wait<CG>(&sh.empty[s], phase ^ 1, &sh, p.status);
-                if (!ok) break;
-                if (elect_one()) {
-                    const uint32_t a = smem_u32(ring + (size_t)s * p.stage_bytes), b = a + kHalves * kHalfBytes;
-                    const int k0 = k * kStepK;
-                    uint32_t bar = CG == 1 ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
-                    if (kMends && K - k0 < kStepK) {   // each CTA counts its own last rows, which have to be mended
-                        uint64_t* end = &sh.ends[ends % kMaxRing];
-                        bar = smem_u32(end);
-                        mbar_arrive_expect_tx(end, bytes);
-                    } else if (rank == 0) {
-                        mbar_arrive_expect_tx(&sh.full[s], CG * bytes);
-                    }
-                    if constexpr (MODE == kGated && CG == 1) {
-                        tile_load<CG>(a, &map_a, k0, f0, 2 * t.e, bar);
-                        tile_load<CG>(a + kHalfBytes, &map_a, k0, f0, 2 * t.e + 1, bar);
-                    } else if constexpr (MODE == kGated) {
-                        tile_load5_pair(a, &map_a, k0, 0, 0, f0 / 8, t.e, bar);
-                    } else if constexpr (MODE == kLinear) {
-                        tile_load<CG>(a, &map_a, k0, f0, t.e, bar);
-                        if (two) tile_load<CG>(a + kHalfBytes, &map_a, k0, f0 + 128, t.e, bar);
-                    } else {
-                        const int y = MODE == kRowsGrad ? k0 : t.row + k0, z = MODE == kRowsGrad ? t.e : 0;
-                        for (int j = 0; j < (two ? 4 : 2); ++j) tile_load<CG>(a + j * 8192, &map_a, f0 + 64 * j, y, z, bar);
-                    }
-                    if constexpr (MODE == kWeightsGrad)
-                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, fb0 + 64 * j, t.row + k0, 0, bar);
-                    else {
-                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, k0, row0 + j * 64, 0, bar);
-                        for (int j = 0; j < small; ++j)
-                            tile_load<CG>(b + large * 8192 + j * 2048, &map_c, k0, row0 + large * 64 + j * 16, 0, bar);
-                    }
-                }
-                __syncwarp();
-                ends += kMends && K - k * kStepK < kStepK;
-                ++used;
-                if (++s == p.stages) {
-                    s = 0;
-                    phase ^= 1;
-                }
-            }
-        }
-        if (CG == 2 && ok)   // the products' last arrivals come to this CTA's barriers: it may not leave before them
-            for (int i = 0; ok && i < p.stages && i < used; ++i) {
-                s = s ? s - 1 : p.stages - 1;
-                if (s == p.stages - 1) phase ^= 1;
-                ok = warp_wait<CG>(&sh.empty[s], phase, &sh, p.status);
-            }
-        else if (!ok) {
-            // nothing may still be on its way into shared memory when the CTA leaves: the last copy of every stage (a pair leaves
-            // together, and the first CTA's barriers count for both)
-            for (int i = 0; rank == 0 && i < p.stages && i < used; ++i) {
-                s = s ? s - 1 : p.stages - 1;
-                if (s == p.stages - 1) phase ^= 1;
-                mbar_wait(&sh.full[s], phase, nullptr);
-            }
-        }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------ products
-        int s = 0, acc = 0;
-        unsigned phase = 0, acc_phase = 0;
-        bool ok = true;
-        for (int id = unit; rank == 0 && ok && walk.find(id, t); id += units) {
-            const int K = MODE == kWeightsGrad ? t.rows : p.K;
-            const int steps = (K + kStepK - 1) / kStepK;
-            if (steps == 0) continue;
-            const bool two = kHalves == 2 && (MODE == kGated || t.f0 + 128 < p.F);
-            const int n = MODE == kWeightsGrad ? 256 : (t.rows + 16 * CG - 1) / (16 * CG) * (16 * CG);
-            const uint32_t idesc = instruction(128 * CG, n, kAcross, MODE == kWeightsGrad);
-            const uint32_t d = tmem + acc * kHalves * p.most;
-            ok = warp_wait<CG>(&sh.acc_empty[acc], acc_phase ^ 1, &sh, p.status);
-            if (!ok) break;
-            tc_fence_after();
-            for (int k = 0; k < steps; ++k) {
-                ok = warp_wait<CG>(&sh.full[s], phase, &sh, p.status);
-                if (!ok) break;
-                uint8_t* stage = ring + (size_t)s * p.stage_bytes;
-                const int left = K - k * kStepK;
-                if constexpr (MODE == kWeightsGrad && CG == 1)
-                    if (left < kStepK) clear_rows(stage, kHalves * 2 + 4, left, lane);
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint32_t a = smem_u32(stage), b = a + kHalves * kHalfBytes;
-                    const int parts = left < kStepK ? (left + 15) / 16 : 4;
-                    for (int j = 0; j < parts; ++j) {
-                        const uint64_t da = kAcross ? operand(a + j * 2048, 8192, 1024) : operand(a + j * 32, 16, 1024);
-                        const uint64_t db = MODE == kWeightsGrad ? operand(b + j * 2048, 8192, 1024) : operand(b + j * 32, 16, 1024);
-                        mma_f16<CG>(d, da, db, idesc, (k | j) != 0);
-                        if (two) mma_f16<CG>(d + p.most, da + (kHalfBytes >> 4), db, idesc, (k | j) != 0);
-                    }
-                    mma_commit<CG>(&sh.empty[s]);
-                    if (k == steps - 1) mma_commit<CG>(&sh.acc_full[acc]);
-                }
-                __syncwarp();
-                if (++s == p.stages) {
-                    s = 0;
-                    phase ^= 1;
-                }
-            }
-            if (++acc == p.accs) {
-                acc = 0;
-                acc_phase ^= 1;
-            }
-        }
-        if (!ok) {   // no product may still be running when the tensor memory is given back
-            if (elect_one()) mma_commit<CG>(&sh.drained);
-            __syncwarp();
-            mbar_wait(&sh.drained, 0, nullptr);
-        }
-    } else if (warp < 2 + kResultWarps) {
+    // (rows with scales keep all of a tile's sums in the registers of the result warps: 384 threads x 168 = 128 x 40 + 256 x 232)
+    if (warp >= kFirstResult) {
         // ------------------------------------------------------------------ results
-        const int quarter = warp & 3, group = (warp - 2) >> 2;   // lanes of tensor memory this warp may read; which columns
-        uint8_t* tiles = results + (MODE == kWeightsGrad ? (warp - 2) * kBlockBytes : group * kGroupBytes);
+        if constexpr (kScaled) registers_up<232>();
+        const int quarter = warp & 3, group = (warp - kFirstResult) >> 2;   // lanes of tensor memory this warp may read; which columns
+        uint8_t* tiles = results + (MODE == kWeightsGrad ? (warp - kFirstResult) * kBlockBytes : group * kGroupBytes);
         int acc = 0, flip = 0;
         unsigned acc_phase = 0;
         for (int id = unit; walk.find(id, t); id += units) {
             const bool empty = MODE == kWeightsGrad && t.rows == 0;
-            if (!empty) {
+            if constexpr (kScaled) {
+                // Rows with scales: the sum over every 128 channels is multiplied with the row's scale of them and added up here, in
+                // 32 bits -- the e4m3 values are bf16 exactly, their products with the scales would be rounded once more.
+                constexpr int kRows = CG == 1 ? 8 : 16, kChunks = CG == 1 ? 4 : 8;   // (64 rows in 4 chunks, 256 in 8, per column group)
+                float sum[kChunks][16];
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[i][j] = 0.0f;
+                group_sync(1 + group, 128);   // (the last tile's results have left the room)
+                float* scales = reinterpret_cast<float*>(tiles);
+                const int me = threadIdx.x - kFirstResult * 32 - group * 128, groups = p.K / 128;
+                const int mine = (me / kRows * 2 + group) * kRows + me % kRows;   // the row whose scales this thread fetches
+                const bool fetches = me < kChunks * kRows && mine < t.rows;
+                const float* from = p.x_scale + (int64_t)(t.row + mine) * groups;
+                float next = fetches ? ld_plain(from) : 0.0f;
+                bool ok = true;
+                for (int g = 0; g < groups; ++g) {
+                    float* here = scales + (g & 1) * 128;
+                    here[me] = next;
+                    if (fetches && g + 1 < groups) next = ld_plain(from + g + 1);
+                    ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
+                    ok = !group_or(1 + group, 128, !ok);   // (also: all scales are there)
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * kHalves * p.most;
+#pragma unroll
+                    for (int i0 = 0; i0 < kChunks; i0 += 4) {   // (a batch's columns are there whether rows use them or not)
+                        const int c = (2 * i0 + group) * kRows;
+                        if (c >= t.rows) break;
+                        float v[4][16];
+                        if constexpr (CG == 1) tmem_ld_pieces(d + c, d + p.most + c, v);
+                        else tmem_ld_pieces(d + c, v);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int j = 0; j < kRows; j += 8) {
+                                const float2 s = *reinterpret_cast<const float2*>(here + (i0 + i) * kRows + j + 2 * (lane & 3));
+#pragma unroll
+                                for (int q = 0; q < (CG == 1 ? 16 : 8); q += 2) {
+                                    // (a pair's piece: halves of lanes, eight values each, of which four of these columns)
+                                    const int at = CG == 1 ? q : q / 4 * 8 + j / 2 + q % 4;
+                                    fma_two(sum[i0 + i] + at, v[i] + at, s);
+                                }
+                            }
+                    }
+                    if (g == groups - 1) {   // the whole sums take the place of the last group's
+#pragma unroll
+                        for (int i = 0; i < kChunks; ++i) {
+                            const int c = (2 * i + group) * kRows;
+                            if (c < t.rows) {
+                                if constexpr (CG == 1) tmem_st_piece(d + c, d + p.most + c, sum[i]);
+                                else tmem_st_piece(d + c, sum[i]);
+                            }
+                        }
+                        break;
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (CG == 1) mbar_arrive(&sh.acc_empty[acc]);
+                        else mbar_arrive_pair_relaxed(first_of_pair(&sh.acc_empty[acc]));
+                    }
+                    if (++acc == p.accs) {
+                        acc = 0;
+                        acc_phase ^= 1;
+                    }
+                }
+                if (!ok) break;
+                group_sync(1 + group, 128);   // (the scales' room is the results')
+            } else if (!empty) {
                 const bool ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
                 // (warps that meet at barriers below leave together)
                 if (MODE == kWeightsGrad ? !ok : group_or(1 + group, 128, !ok)) break;
@@ -341,7 +292,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
                 __syncwarp();
                 if (lane == 0) {
                     if constexpr (CG == 1) mbar_arrive(&sh.acc_empty[acc]);
-                    else mbar_arrive_pair(first_of_pair(&sh.acc_empty[acc]));
+                    else mbar_arrive_pair_relaxed(first_of_pair(&sh.acc_empty[acc]));
                 }
             };
             if constexpr (MODE == kWeightsGrad) {
@@ -375,14 +326,14 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
             } else {
                 // one CTA and the gated block: gate and up of a feature in the same lane, in two accumulators, eight rows at a time; a
                 // pair: eight lanes gate, the next eight lanes up of the same features, so that a lane finishes every second row
-                constexpr int kRows = MODE == kGated && CG == 1 ? 8 : 16;
-                constexpr int kWidth = MODE == kGated && CG == 2 ? 64 : 128, kPitch = kWidth == 64 ? kNarrow : kWide;
+                constexpr int kRows = gated(MODE) && CG == 1 ? 8 : 16;
+                constexpr int kWidth = gated(MODE) && CG == 2 ? 64 : 128, kPitch = kWidth == 64 ? kNarrow : kWide;
                 constexpr int kTile = kRows * kPitch, kVecs = kWidth / 8, kPasses = kRows * kVecs / 128;
-                const int me = threadIdx.x - 64 - group * 128;   // thread of the column group
-                for (int h = 0; h < (MODE == kGated ? 1 : kHalves); ++h) {
-                    const int f0 = t.f0 + (MODE == kGated ? rank * kWidth : (h + rank) * 128);
+                const int me = threadIdx.x - kFirstResult * 32 - group * 128;   // thread of the column group
+                for (int h = 0; h < (gated(MODE) ? 1 : kHalves); ++h) {
+                    const int f0 = t.f0 + (gated(MODE) ? rank * kWidth : (h + rank) * 128);
                     if (f0 >= p.F) break;
-                    const int col = MODE == kGated && CG == 2 ? quarter * 16 + (lane >> 4) * 8 + (lane & 7) : quarter * 32 + lane;
+                    const int col = gated(MODE) && CG == 2 ? quarter * 16 + (lane >> 4) * 8 + (lane & 7) : quarter * 32 + lane;
                     // whole rows' pieces, 16 bytes per thread: rows and features of this thread's vectors
                     const int vec_f = f0 + me % kVecs * 8, vec_row = me / kVecs;
                     const bool vec_in = vec_f < p.F;
@@ -409,13 +360,13 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
                         if (p.residual) fetch(group * kRows);
                     }
                     for (int c = group * kRows; c < t.rows; c += 2 * kRows) {
-                        const bool last = c + 2 * kRows >= t.rows && (MODE == kGated || h == kHalves - 1 || f0 + 128 >= p.F);
+                        const bool last = c + 2 * kRows >= t.rows && (gated(MODE) || h == kHalves - 1 || f0 + 128 >= p.F);
                         uint8_t* tile = tiles + (p.pre ? 0 : flip * kTile);
                         float v[16];
-                        if constexpr (MODE == kGated && CG == 1) tmem_ld8x2(d + c, d + p.most + c, v, v + 8);
+                        if constexpr (gated(MODE) && CG == 1) tmem_ld8x2(d + c, d + p.most + c, v, v + 8);
                         else tmem_ld16(d + h * p.most + c, v);
                         give_back(last);
-                        if constexpr (MODE == kGated) {
+                        if constexpr (gated(MODE)) {
                             float g[8], u[8];
                             const bool up = lane & 8;
 #pragma unroll
@@ -474,8 +425,8 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
                         group_sync(1 + group, 128);
                         put_out(p.out, p.F, tile, c);
                         if (p.pre) {
-                            put_out(p.pre, MODE == kGated ? 2 * p.F : p.F, tile + kTile, c);
-                            if (MODE == kGated) put_out(p.pre + p.F, 2 * p.F, tile + 2 * kTile, c);
+                            put_out(p.pre, gated(MODE) ? 2 * p.F : p.F, tile + kTile, c);
+                            if (gated(MODE)) put_out(p.pre + p.F, 2 * p.F, tile + 2 * kTile, c);
                             group_sync(1 + group, 128);
                         }
                         flip ^= 1;   // (the other tile's readers have met at a barrier since)
@@ -489,31 +440,167 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
             }
         }
         if constexpr (MODE == kWeightsGrad) bulk_wait_all<0>();
-    } else if constexpr (kMends) {
+    } else {
+    if constexpr (kScaled) registers_down<40>();
+    if (warp == 0) {
+        // ------------------------------------------------------------------ loads
+        int s = 0, used = 0, ends = 0;
+        unsigned phase = 0;
+        bool ok = true;
+        for (int id = unit; ok && walk.find(id, t); id += units) {
+            const int K = MODE == kWeightsGrad ? t.rows : p.K;
+            const int steps = (K + kStepK - 1) / kStepK;
+            const bool two = kHalves == 2 && (gated(MODE) || t.f0 + 128 < p.F);
+            const int f0 = t.f0 + rank * (gated(MODE) ? 64 : 128), fb0 = t.fb0 + rank * 128;
+            // (in a pair each CTA brings one half of the rows, or of x's features)
+            const int mine = CG == 1 ? t.rows : (t.rows + 31) / 32 * 16, row0 = t.row + rank * mine;
+            // (boxes of 64 and of 16 rows: a copy costs the loading warp some 55 cycles, eight copies of 16 rows nearly the whole step)
+            const int small = MODE == kWeightsGrad ? 0 : (mine + 15) / 16 % 4, large = MODE == kWeightsGrad ? 4 / CG : (mine + 15) / 64;
+            const unsigned bytes = (two ? 2 : 1) * kHalfBytes + large * 8192 + small * 2048;
+            const int passes = MODE == kWeightsGrad ? p.planes : 1;
+            for (int k = 0, plane = 0; k < steps; k += plane == passes - 1, plane = plane == passes - 1 ? 0 : plane + 1) {
+                ok = warp_wait<CG>(&sh.empty[s], phase ^ 1, &sh, p.status);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t a = smem_u32(ring + (size_t)s * p.stage_bytes), b = a + kHalves * kHalfBytes;
+                    const int k0 = k * kStepK;
+                    uint32_t bar = CG == 1 ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
+                    if (kMends && K - k0 < kStepK) {   // each CTA counts its own last rows, which have to be mended
+                        uint64_t* end = &sh.ends[ends % kMaxRing];
+                        bar = smem_u32(end);
+                        mbar_arrive_expect_tx(end, bytes);
+                    } else if (rank == 0) {
+                        mbar_arrive_expect_tx(&sh.full[s], CG * bytes);
+                    }
+                    if constexpr (gated(MODE) && CG == 1) {
+                        tile_load<CG>(a, &map_a, k0, f0, 2 * t.e, bar);
+                        tile_load<CG>(a + kHalfBytes, &map_a, k0, f0, 2 * t.e + 1, bar);
+                    } else if constexpr (gated(MODE)) {
+                        tile_load5_pair(a, &map_a, k0, 0, 0, f0 / 8, t.e, bar);
+                    } else if constexpr (MODE == kLinear) {
+                        tile_load<CG>(a, &map_a, k0, f0, t.e, bar);
+                        if (two) tile_load<CG>(a + kHalfBytes, &map_a, k0, f0 + 128, t.e, bar);
+                    } else {
+                        const int y = MODE == kRowsGrad ? k0 : t.row + k0, z = MODE == kRowsGrad ? t.e : 0;
+                        for (int j = 0; j < (two ? 4 : 2); ++j) tile_load<CG>(a + j * 8192, &map_a, f0 + 64 * j, y, z, bar);
+                    }
+                    if constexpr (MODE == kWeightsGrad)
+                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, fb0 + 64 * j, t.row + k0, plane, bar);
+                    else {
+                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, k0, row0 + j * 64, 0, bar);
+                        for (int j = 0; j < small; ++j)
+                            tile_load<CG>(b + large * 8192 + j * 2048, &map_c, k0, row0 + large * 64 + j * 16, 0, bar);
+                    }
+                }
+                __syncwarp();
+                ends += kMends && K - k * kStepK < kStepK;
+                ++used;
+                if (++s == p.stages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+        if (CG == 2 && ok)   // the products' last arrivals come to this CTA's barriers: it may not leave before them
+            for (int i = 0; ok && i < p.stages && i < used; ++i) {
+                s = s ? s - 1 : p.stages - 1;
+                if (s == p.stages - 1) phase ^= 1;
+                ok = warp_wait<CG>(&sh.empty[s], phase, &sh, p.status);
+            }
+        else if (!ok) {
+            // nothing may still be on its way into shared memory when the CTA leaves: the last copy of every stage (a pair leaves
+            // together, and the first CTA's barriers count for both)
+            for (int i = 0; rank == 0 && i < p.stages && i < used; ++i) {
+                s = s ? s - 1 : p.stages - 1;
+                if (s == p.stages - 1) phase ^= 1;
+                mbar_wait(&sh.full[s], phase, nullptr);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ products
+        int s = 0, acc = 0;
+        unsigned phase = 0, acc_phase = 0;
+        bool ok = true;
+        for (int id = unit; rank == 0 && ok && walk.find(id, t); id += units) {
+            const int K = MODE == kWeightsGrad ? t.rows : p.K;
+            const int steps = (K + kStepK - 1) / kStepK;
+            if (steps == 0) continue;
+            const bool two = kHalves == 2 && (gated(MODE) || t.f0 + 128 < p.F);
+            const int n = MODE == kWeightsGrad ? 256 : (t.rows + 16 * CG - 1) / (16 * CG) * (16 * CG);
+            const uint32_t idesc = instruction(128 * CG, n, kAcross, MODE == kWeightsGrad);
+            uint32_t d = 0;
+            const int passes = MODE == kWeightsGrad ? p.planes : 1;
+            for (int k = 0, plane = 0; k < steps; k += plane == passes - 1, plane = plane == passes - 1 ? 0 : plane + 1) {
+                // (rows with scales: every group of 128 channels is a sum of its own, two steps)
+                const bool opens = kScaled ? k % 2 == 0 : k + plane == 0, closes = kScaled ? k % 2 != 0 : k == steps - 1 && plane == passes - 1;
+                if (opens) {
+                    ok = warp_wait<CG>(&sh.acc_empty[acc], acc_phase ^ 1, &sh, p.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    d = tmem + acc * kHalves * p.most;
+                }
+                ok = warp_wait<CG>(&sh.full[s], phase, &sh, p.status);
+                if (!ok) break;
+                uint8_t* stage = ring + (size_t)s * p.stage_bytes;
+                const int left = K - k * kStepK;
+                if constexpr (MODE == kWeightsGrad && CG == 1)
+                    if (left < kStepK) clear_rows(stage, kHalves * 2 + 4, left, lane);
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t a = smem_u32(stage), b = a + kHalves * kHalfBytes;
+                    const int parts = left < kStepK ? (left + 15) / 16 : 4;
+                    for (int j = 0; j < parts; ++j) {
+                        const uint64_t da = kAcross ? operand(a + j * 2048, 8192, 1024) : operand(a + j * 32, 16, 1024);
+                        const uint64_t db = MODE == kWeightsGrad ? operand(b + j * 2048, 8192, 1024) : operand(b + j * 32, 16, 1024);
+                        const bool add = !opens || j != 0;
+                        mma_f16<CG>(d, da, db, idesc, add);
+                        if (two) mma_f16<CG>(d + p.most, da + (kHalfBytes >> 4), db, idesc, add);
+                    }
+                    mma_commit<CG>(&sh.empty[s]);
+                    if (closes) mma_commit<CG>(&sh.acc_full[acc]);
+                }
+                __syncwarp();
+                if (++s == p.stages) {
+                    s = 0;
+                    phase ^= 1;
+                }
+                if (closes && ++acc == p.accs) {
+                    acc = 0;
+                    acc_phase ^= 1;
+                }
+            }
+        }
+        if (!ok) {   // no product may still be running when the tensor memory is given back
+            if (elect_one()) mma_commit<CG>(&sh.drained);
+            __syncwarp();
+            mbar_wait(&sh.drained, 0, nullptr);
+        }
+    } else if (kMends && warp == 2) {
         // ------------------------------------------------------------------ last rows of a segment in the weights' gradient
         // Both CTAs clear what is behind them in their own operands; the second tells the first, and the first completes the stage
         // that its products wait for.  (Done for every step, the arrival at the other CTA alone took more than twice a step's time.)
         int s = 0, ends = 0;
         bool ok = true;
         for (int id = unit; ok && walk.find(id, t); id += units) {
-            s += (t.rows + kStepK - 1) / kStepK;
+            s += t.rows / kStepK * p.planes;
             const int left = t.rows % kStepK;
-            if (!left) continue;
-            const int at = (s - 1) % p.stages, end = ends % kMaxRing;
-            const unsigned phase = ends / kMaxRing & 1;
-            ok = warp_wait<CG>(&sh.ends[end], phase, &sh, p.status);
-            if (!ok) break;
-            clear_rows(ring + (size_t)at * p.stage_bytes, 4, left, lane);
-            if (rank == 0) {
-                ok = warp_wait<CG>(&sh.cleared[end], phase, &sh, p.status);
+            for (int plane = 0; left && plane < p.planes; ++plane, ++s, ++ends) {
+                const int at = s % p.stages, end = ends % kMaxRing;
+                const unsigned phase = ends / kMaxRing & 1;
+                ok = warp_wait<CG>(&sh.ends[end], phase, &sh, p.status);
                 if (!ok) break;
-                if (lane == 0) mbar_arrive(&sh.full[at]);
-            } else if (lane == 0) {
-                mbar_arrive_pair(first_of_pair(&sh.cleared[end]));
+                clear_rows(ring + (size_t)at * p.stage_bytes, 4, left, lane);
+                if (rank == 0) {
+                    ok = warp_wait<CG>(&sh.cleared[end], phase, &sh, p.status);
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive(&sh.full[at]);
+                } else if (lane == 0) {
+                    mbar_arrive_pair(first_of_pair(&sh.cleared[end]));
+                }
             }
-            ++ends;
             s %= p.stages;
         }
+    }
     }
     tc_fence_before();
     __syncwarp();
@@ -528,29 +615,56 @@ __global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const
 
 constexpr int kRowThreads = 256;
 
-// Rows quantised by an FP8 dispatch as bf16: e4m3 times the scale of its 128 channels, rounded once.  One block takes every
-// gridDim.x-th row of an expert.
-__global__ void __launch_bounds__(kRowThreads) widen_kernel(const uint8_t* q, const float* scale, uint16_t* out, int H, Segments seg) {
+// Rows quantised by an FP8 dispatch as bf16.  Forward: the e4m3 values alone, which bf16 holds exactly (their scales are applied to the
+// sums).  Weights' gradient, whose sum runs over rows with different scales: value times scale as the sum of two bf16 numbers,
+// the second in the second half of the scratch (off by 2^-17 of the value; one bf16 would be off by 2^-9).  A warp per row, eight
+// channels per lane: 8-byte loads, 16-byte stores, six of each on their way.
+constexpr int kWidenAhead = 6;
+template <bool SPLIT>
+__global__ void __launch_bounds__(kRowThreads) widen_kernel(const uint8_t* q, const float* scale, uint16_t* out, int64_t plane, int H,
+                                                           Segments seg) {
     griddep_wait();
+    const int lane = threadIdx.x & 31, warps = kRowThreads / 32;
     int first, rows;
     for (int e = blockIdx.y; e < seg.E; e += gridDim.y) {
         segment(seg, e, first, rows);
-        for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+        for (int r = blockIdx.x * warps + (threadIdx.x >> 5); r < rows; r += gridDim.x * warps) {
             const int64_t row = first + r;
-            for (int c = threadIdx.x * 16; c < H; c += kRowThreads * 16) {
-                const uint4 in = *reinterpret_cast<const uint4*>(q + row * H + c);
-                const float s = ld_plain(scale + row * (H / 128) + c / 128);
-                const uint32_t w[4] = {in.x, in.y, in.z, in.w};
-                float f[16];
+            const uint8_t* from = q + row * H;
+            for (int c0 = lane * 8; c0 < H; c0 += 256 * kWidenAhead) {
+                uint2 in[kWidenAhead];
+                float s[kWidenAhead];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
-                    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                    f[2 * i] = v.x * s;
-                    f[2 * i + 1] = v.y * s;
+                for (int i = 0; i < kWidenAhead; ++i) {
+                    const int c = c0 + i * 256;
+                    if (c < H) {
+                        in[i] = *reinterpret_cast<const uint2*>(from + c);
+                        if (SPLIT) s[i] = ld_plain(scale + row * (H / 128) + c / 128);
+                    }
                 }
-                st_vec(out + row * H + c, pack8(f));
-                st_vec(out + row * H + c + 8, pack8(f + 8));
+#pragma unroll
+                for (int i = 0; i < kWidenAhead; ++i) {
+                    const int c = c0 + i * 256;
+                    if (c >= H) break;
+                    float f[8];
+                    const uint32_t w[2] = {in[i].x, in[i].y};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j >> 1] >> (16 * (j & 1))), __NV_E4M3);
+                        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                        f[2 * j] = SPLIT ? v.x * s[i] : v.x;
+                        f[2 * j + 1] = SPLIT ? v.y * s[i] : v.y;
+                    }
+                    const uint4 high = pack8(f);
+                    st_vec(out + row * H + c, high);
+                    if (SPLIT) {
+                        float back[8];
+                        unpack8(high, back);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[j] -= back[j];
+                        st_vec(out + plane + row * H + c, pack8(f));
+                    }
+                }
             }
         }
     }
@@ -747,7 +861,7 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     static std::atomic<int> granted[kAttrDevices];
     e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, CG>), smem, granted);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE, CG), (size_t)smem, st, false, CG, a, b, c, p);
+    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, kGemmThreads, (size_t)smem, st, false, CG, a, b, c, p);
 }
 
 // The segments of a call are not known to the host, their capacity is.
@@ -772,21 +886,18 @@ Segments segments_of(const ubep_expert_rows_t& r) {
     return Segments{r.offset, r.count, r.num_experts, r.num_experts / r.num_ranks, r.rows_per_rank_cap};
 }
 
-// x as bf16 rows: itself, or widened into the scratch.
-cudaError_t rows_in(const ubep_expert_rows_t& r, const void* x, const float* x_scale, void* scratch, int K, const void** out,
-                    cudaStream_t st, int* launches) {
-    *out = x;
-    if (!x_scale) return cudaSuccess;
+// FP8 rows as bf16 in the scratch.
+template <bool SPLIT>
+cudaError_t widen(const ubep_expert_rows_t& r, const void* x, const float* x_scale, void* scratch, int H, cudaStream_t st, int* launches) {
     DeviceFacts dev;
     cudaError_t e = device_facts(&dev);
     if (e != cudaSuccess) return e;
     dim3 grid = row_grid(r, dev);
-    widen_kernel<<<grid, kRowThreads, 0, st>>>(static_cast<const uint8_t*>(x), x_scale, static_cast<uint16_t*>(scratch), K, segments_of(r));
-    *out = scratch;
+    grid.x = (grid.x + kRowThreads / 32 - 1) / (kRowThreads / 32);
     ++*launches;
-    return cudaGetLastError();
+    return launch_overlapped(widen_kernel<SPLIT>, grid, kRowThreads, 0, st, false, 1, static_cast<const uint8_t*>(x), x_scale,
+                             static_cast<uint16_t*>(scratch), (int64_t)all_rows(r) * H, H, segments_of(r));
 }
-
 
 // dx[row, k] = sum_n dz[row, n] w[e, n, k]
 cudaError_t rows_grad(const ubep_expert_rows_t& r, const void* dz, const void* w, int K, int N, void* grad_x, cudaStream_t st) {
@@ -804,16 +915,18 @@ cudaError_t rows_grad(const ubep_expert_rows_t& r, const void* dz, const void* w
 }
 
 // dw[e, n, k] = sum_row dz[row, n] x[row, k]
-cudaError_t weights_grad(const ubep_expert_rows_t& r, const void* dz, const void* x, int K, int N, void* grad_w, cudaStream_t st) {
+cudaError_t weights_grad(const ubep_expert_rows_t& r, const void* dz, const void* x, int planes, int K, int N, void* grad_w,
+                         cudaStream_t st) {
     Product p{};
     p.seg = segments_of(r);
     p.F = N;
     p.FB = K;
     p.most = 256;
+    p.planes = planes;
     p.out = static_cast<uint16_t*>(grad_w);
     p.status = r.status;
     CUtensorMap a, b, out;
-    if (!make_map(&a, dz, N, all_rows(r), 1, 64) || !make_map(&b, x, K, all_rows(r), 1, 64) || !make_map(&out, grad_w, K, N, r.num_experts, 32))
+    if (!make_map(&a, dz, N, all_rows(r), 1, 64) || !make_map(&b, x, K, all_rows(r), planes, 64) || !make_map(&out, grad_w, K, N, r.num_experts, 32))
         return cudaErrorInvalidValue;
     return in_pairs(r) ? launch_product<kWeightsGrad, 2>(a, b, out, p, st) : launch_product<kWeightsGrad, 1>(a, b, out, p, st);
 }
@@ -822,10 +935,11 @@ cudaError_t weights_grad(const ubep_expert_rows_t& r, const void* dz, const void
 
 cudaError_t launch_expert_gated(const ubep_expert_rows_t& r, const void* x, const float* x_scale, const void* w, int H, int I, int act,
                                 void* h, void* pre, void* scratch, cudaStream_t st, int* launches) {
-    const void* rows;
-    cudaError_t e = rows_in(r, x, x_scale, scratch, H, &rows, st, launches);
+    const void* rows = x_scale ? scratch : x;
+    cudaError_t e = x_scale ? widen<false>(r, x, x_scale, scratch, H, st, launches) : cudaSuccess;
     if (e != cudaSuccess) return e;
     Product p{};
+    p.x_scale = x_scale;
     p.seg = segments_of(r);
     p.F = I;
     p.K = H;
@@ -839,7 +953,10 @@ cudaError_t launch_expert_gated(const ubep_expert_rows_t& r, const void* x, cons
     if (!(pairs ? make_gated_map(&a, w, H, I, r.num_experts) : make_map(&a, w, H, I, 2 * (uint64_t)r.num_experts, 128)) ||
         !make_rows_maps(&b, &c, rows, H, r))
         return cudaErrorInvalidValue;
-    e = pairs ? launch_product<kGated, 2>(a, b, c, p, st) : launch_product<kGated, 1>(a, b, c, p, st);
+    if (x_scale)
+        e = pairs ? launch_product<kGatedScaled, 2>(a, b, c, p, st) : launch_product<kGatedScaled, 1>(a, b, c, p, st);
+    else
+        e = pairs ? launch_product<kGated, 2>(a, b, c, p, st) : launch_product<kGated, 1>(a, b, c, p, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -847,8 +964,7 @@ cudaError_t launch_expert_gated(const ubep_expert_rows_t& r, const void* x, cons
 cudaError_t launch_expert_gated_backward(const ubep_expert_rows_t& r, const void* x, const float* x_scale, const void* w, const void* pre,
                                          const void* grad_h, int H, int I, int act, void* grad_pre, void* grad_x, void* grad_w,
                                          void* scratch, cudaStream_t st, int* launches) {
-    const void* rows;
-    cudaError_t e = rows_in(r, x, grad_w ? x_scale : nullptr, scratch, H, &rows, st, launches);
+    cudaError_t e = grad_w && x_scale ? widen<true>(r, x, x_scale, scratch, H, st, launches) : cudaSuccess;
     if (e != cudaSuccess) return e;
     DeviceFacts dev;
     e = device_facts(&dev);
@@ -864,7 +980,7 @@ cudaError_t launch_expert_gated_backward(const ubep_expert_rows_t& r, const void
         ++*launches;
     }
     if (grad_w) {
-        e = weights_grad(r, grad_pre, rows, H, 2 * I, grad_w, st);
+        e = weights_grad(r, grad_pre, x_scale ? scratch : x, x_scale ? 2 : 1, H, 2 * I, grad_w, st);
         if (e != cudaSuccess) return e;
         ++*launches;
     }
@@ -924,7 +1040,7 @@ cudaError_t launch_expert_linear_backward(const ubep_expert_rows_t& r, const voi
         ++*launches;
     }
     if (grad_w) {
-        e = weights_grad(r, dz, x, K, N, grad_w, st);
+        e = weights_grad(r, dz, x, 1, K, N, grad_w, st);
         if (e != cudaSuccess) return e;
         ++*launches;
     }

@@ -14,10 +14,10 @@ namespace ubep {
 // error instead of CTAs spinning until their bounded waits run out) and starts the grid only
 // when every CTA has a place.  Such a kernel is not launched ahead of its predecessor's end.
 template <typename... KArgs, typename... Args>
-static cudaError_t launch_overlapped(void (*kern)(KArgs...), int grid, int block, size_t smem, cudaStream_t st,
+static cudaError_t launch_overlapped(void (*kern)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t st,
                                      bool together, int cluster, Args... args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

@@ -521,7 +521,7 @@ PyObject* py_gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
             gp = room.data_ptr();
         }
         Output gx(a[10], "grad_x", at, at::kBFloat16, {x.R, x.cap, x.width}, true), gw(a[11], "grad_w", at, at::kBFloat16, w.sizes(), true);
-        if (x.scale && gw.ptr) scratch = at.scratch({x.R, x.cap, x.width}, at::kBFloat16);
+        if (x.scale && gw.ptr) scratch = at.scratch({2, x.R, x.cap, x.width}, at::kBFloat16);
         const void *px = x.t.data_ptr(), *pw = w.data_ptr(), *pp = pre.data_ptr(), *ph = gh.data_ptr();
         void* ps = scratch.defined() ? scratch.data_ptr() : nullptr;
         const int32_t H = narrow(x.width, "x"), Ii = narrow(I, "w");

@@ -157,32 +157,57 @@ def test_gated_wide(act, H, I):
     R.check("h", out, want, tol)
 
 
-@pytest.mark.parametrize("segments", ["small", "edges", "over_the_end"])
-def test_gated_takes_fp8_rows(segments):
-    R = Rows(segments)
-    gen = _gen(5)
-    H, I = 384, 136
+def _fp8(R, gen, H):
+    """e4m3 rows with a scale per 128 channels, and what they stand for; rows of no segment have no number as their scale."""
     x = torch.randn((R.R, R.cap, H), generator=gen, device="cuda")
     scale = torch.rand((R.R, R.cap, H // 128), generator=gen, device="cuda") * 0.02 + 0.001
     q = (x / scale.repeat_interleave(128, dim=2)).clamp(-448, 448).to(torch.float8_e4m3fn)
     scale[~R.mine] = float("nan")
-    w = _weights(gen, R.E, 2, I, H)
-    rows = (q.float().double() * scale.double().repeat_interleave(128, dim=2))
+    rows = q.float().double() * scale.double().repeat_interleave(128, dim=2)
     rows[~R.mine] = 0
-    # the rows are rounded to bf16 for the products: half a step of each
-    _, pre_tol, want, tol = gated_exact(R, rows, w, "silu")
-    pre_size = f64(q, (2, I))
-    for e, r, a, b in R.each():
-        for i in range(2):
-            pre_size[r, a:b, i] = rows[r, a:b].abs() @ w[e, i].double().abs().T
-    pre, _, _, _ = gated_exact(R, rows, w, "silu")
-    g, u = pre[:, :, 0], pre[:, :, 1]
-    dg, du = HALF * pre_size[:, :, 0], HALF * pre_size[:, :, 1]
-    tol = tol + 1.13 * dg * (u.abs() + du) + act_exact(g, "silu")[0].abs() * du
+    return q, scale, rows
+
+
+@pytest.mark.parametrize("segments", SEGMENTS)
+@pytest.mark.parametrize("H,I", [(128, 8), (384, 136), (1024, 264)])
+def test_gated_takes_fp8_rows(segments, H, I):
+    # (the values are multiplied as they are and the sums scaled in 32 bits: no rounding to bf16 on the way)
+    R = Rows(segments)
+    gen = _gen(5)
+    q, scale, rows = _fp8(R, gen, H)
+    w = _weights(gen, R.E, 2, I, H)
+    want_pre, pre_tol, want, tol = gated_exact(R, rows, w, "silu")
     for t in (q, q.view(torch.uint8)):
-        out = R.filled(I)
-        B.expert_gated(R.rows, t, w, x_scale=scale, out=out)
-        R.check("h", out, want, tol * 1.01)
+        out, pre = R.filled(I), R.filled(2, I)
+        B.expert_gated(R.rows, t, w, x_scale=scale, out=out, pre=pre)
+        R.check("pre", pre, want_pre, pre_tol)
+        R.check("h", out, want, tol)
+        again = R.filled(I)
+        B.expert_gated(R.rows, t, w, x_scale=scale, out=again)
+        assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("segments", SEGMENTS)
+@pytest.mark.parametrize("H,I", [(128, 72), (640, 264)])
+def test_gated_backward_takes_fp8_rows(segments, H, I):
+    # (rows as the sum of two bf16 numbers, off by half a step of the second: 2^-17 of the value)
+    R = Rows(segments)
+    gen = _gen(6)
+    q, scale, rows = _fp8(R, gen, H)
+    w, pre, grad = _weights(gen, R.E, 2, I, H), R.randn(gen, 2, I), R.randn(gen, I)
+    g, u, dh = (torch.where(R.mine[..., None], t.double(), 0.0) for t in (pre[:, :, 0], pre[:, :, 1], grad))
+    v, s = act_exact(g, "silu")
+    d = torch.cat((dh * u * s, dh * v), -1)
+    size = torch.cat((dh * u * (1 + g.abs()), dh * (1 + g.abs())), -1).abs() * 2.0 ** -18
+    gx, tx, gw, tw = grads_exact(R, rows, w.view(R.E, 2 * I, H), d, H)
+    _, sx, _, sw = grads_exact(R, rows, w.view(R.E, 2 * I, H), size / HALF, H)
+    grad_x, grad_w = R.filled(H), torch.full_like(w, FILL)
+    B.expert_gated_backward(R.rows, q, w, pre, grad, x_scale=scale, grad_x=grad_x, grad_w=grad_w)
+    R.check("grad_x", grad_x, gx, tx + sx)
+    # (two products per row: twice the terms of the sum)
+    check_all("grad_w", grad_w.view(R.E, 2 * I, H), gw, tw * (1 + 2.0 ** -8) + sw + R.cap * SUM * tw / HALF)
+    only = B.expert_gated_backward(R.rows, q, w, pre, grad, x_scale=scale, grad_w=False)[0]
+    assert torch.equal(only[R.mine], grad_x[R.mine])
 
 
 @pytest.mark.parametrize("segments", SEGMENTS)
