@@ -31,21 +31,23 @@ namespace {
 enum { kGated = 0, kLinear = 1, kRowsGrad = 2, kWeightsGrad = 3, kGatedScaled = 4 };
 __host__ __device__ constexpr bool gated(int mode) { return mode == kGated || mode == kGatedScaled; }   // kGatedScaled: rows of an FP8 dispatch
 
-// A warpgroup with a loading warp, a multiplying warp and (weights' gradient in pairs) one that mends the last rows; two for the results.
-constexpr int kGemmThreads = 384;
+// A warpgroup with a loading warp, a multiplying warp and (weights' gradient in pairs) one that mends the last rows; the others turn
+// sums into results: in groups of four warps, which share the tile's columns.
 constexpr int kFirstResult = 4;
-constexpr int kResultWarps = 8;
+__host__ __device__ constexpr int result_groups(int) { return 2; }
+__host__ __device__ constexpr int gemm_threads(int mode) { return 32 * (kFirstResult + 4 * result_groups(mode)); }
 constexpr int kStepK = 64;               // of the contraction per stage: 128 bytes of bf16, the swizzle's width
 constexpr int kHalfBytes = 128 * 128;    // 128 features of one stage
 constexpr int kMaxRing = 8;
+constexpr int kColumns = 512;            // tensor memory: all of it (one CTA per SM)
 // Finished results go through shared memory, so that whole lines are written.  Rows: tiles of 16 rows per column group, two of them
 // in turn, or one beside those of the saved products; weights' gradient: a tile of 32 x 64 per warp, one tensor copy each.
 constexpr int kWide = 272;               // bytes per row of 128 results (16 to spread the banks), 16 rows per tile, 8 of them
 constexpr int kNarrow = 160;             // ... of 64 (the gated block in pairs): two neighbouring rows in different banks
-constexpr int kGroupBytes = 2 * 16 * kWide;
 constexpr int kBlockBytes = 32 * 128;
-constexpr int out_bytes(int mode) { return mode == kWeightsGrad ? kResultWarps * kBlockBytes : 2 * kGroupBytes; }
-constexpr int kColumns = 512;            // tensor memory: all of it (one CTA per SM)
+__host__ __device__ constexpr int tile_bytes(int mode, int cg) {
+    return mode == kWeightsGrad ? 4 * kBlockBytes : gated(mode) ? (cg == 1 ? 8 * kWide : 16 * kNarrow) : 16 * kWide;
+}
 
 struct Product {
     Segments seg;
@@ -54,6 +56,7 @@ struct Product {
     int FB;          // weights' gradient: features of x
     int most;        // rows per tile at most; columns of one accumulator
     int stages, stage_bytes, accs;
+    int tiles;       // of results per column group
     int act;
     uint16_t *out, *pre;
     const uint16_t *bias, *residual;
@@ -88,6 +91,20 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity, Shared
         if (status) report(status, kErrTimeout);
     }
     return false;
+}
+
+// The same of one thread.
+template <int CG>
+__device__ __forceinline__ bool thread_wait(uint64_t* bar, unsigned parity, Shared* sh, int32_t* status) {
+    if (CG == 1 ? mbar_try_wait(bar, parity, 1000u) : mbar_try_wait_pair(bar, parity, 1000u)) return true;
+    const unsigned long long t_end = global_ns() + kWaitLimitNs;
+    while (!(CG == 1 ? mbar_try_wait(bar, parity, 1000u) : mbar_try_wait_pair(bar, parity, 1000u)))
+        if (*(volatile int*)&sh->abort || global_ns() > t_end) {
+            *(volatile int*)&sh->abort = 1;
+            if (status) report(status, kErrTimeout);
+            return false;
+        }
+    return true;
 }
 
 // Place of a tile: expert, rows and features.
@@ -148,15 +165,19 @@ __device__ __forceinline__ uint4 ld_vec(const uint16_t* p) { return *reinterpret
 __device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
 template <int MODE, int CG>
-__global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
+__global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                           const __grid_constant__ CUtensorMap map_b,
                                                                           const __grid_constant__ CUtensorMap map_c, const Product p) {
     extern __shared__ uint8_t dynamic[];
     __shared__ Shared sh;
     constexpr int kHalves = CG == 1 ? 2 : 1;                              // tiles of 128 features that this CTA multiplies with one tile of rows
     constexpr bool kAcross = MODE == kRowsGrad || MODE == kWeightsGrad;   // the features' operand
-    constexpr bool kMends = MODE == kWeightsGrad && CG == 2;
+    constexpr bool kMends = MODE == kWeightsGrad;
     constexpr bool kScaled = MODE == kGatedScaled;
+    constexpr int kGroups = result_groups(MODE), kTile = tile_bytes(MODE, CG);
+    // Rows with scales keep a tile's sums in the result warps' registers, which get some of the others'.
+    constexpr bool kSplits = kScaled;
+    constexpr int kFewRegisters = 40, kManyRegisters = 232;   // 384 threads x 168 = 128 x 40 + 256 x 232
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
     uint8_t* results = ring + (size_t)p.stages * p.stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -172,7 +193,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.acc_full[i], 1);
-            mbar_init(&sh.acc_empty[i], kResultWarps * CG);
+            mbar_init(&sh.acc_empty[i], 4 * kGroups * CG);
         }
         mbar_init(&sh.drained, 1);
         sh.abort = 0;
@@ -197,12 +218,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
     const int unit = blockIdx.x / CG, units = gridDim.x / CG;
     Walk<MODE, CG> walk(p);
     Tile t;
-    // (rows with scales keep all of a tile's sums in the registers of the result warps: 384 threads x 168 = 128 x 40 + 256 x 232)
     if (warp >= kFirstResult) {
         // ------------------------------------------------------------------ results
-        if constexpr (kScaled) registers_up<232>();
+        if constexpr (kSplits) registers_up<kManyRegisters>();
         const int quarter = warp & 3, group = (warp - kFirstResult) >> 2;   // lanes of tensor memory this warp may read; which columns
-        uint8_t* tiles = results + (MODE == kWeightsGrad ? (warp - kFirstResult) * kBlockBytes : group * kGroupBytes);
+        uint8_t* tiles = results + (MODE == kWeightsGrad ? (warp - kFirstResult) * kBlockBytes : group * p.tiles * kTile);
         int acc = 0, flip = 0;
         unsigned acc_phase = 0;
         for (int id = unit; walk.find(id, t); id += units) {
@@ -210,7 +230,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
             if constexpr (kScaled) {
                 // Rows with scales: the sum over every 128 channels is multiplied with the row's scale of them and added up here, in
                 // 32 bits -- the e4m3 values are bf16 exactly, their products with the scales would be rounded once more.
-                constexpr int kRows = CG == 1 ? 8 : 16, kChunks = CG == 1 ? 4 : 8;   // (64 rows in 4 chunks, 256 in 8, per column group)
+                constexpr int kRows = CG == 1 ? 8 : 16, kChunks = (CG == 1 ? 64 : 256) / kRows / kGroups;
                 float sum[kChunks][16];
 #pragma unroll
                 for (int i = 0; i < kChunks; ++i)
@@ -219,29 +239,40 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                 group_sync(1 + group, 128);   // (the last tile's results have left the room)
                 float* scales = reinterpret_cast<float*>(tiles);
                 const int me = threadIdx.x - kFirstResult * 32 - group * 128, groups = p.K / 128;
-                const int mine = (me / kRows * 2 + group) * kRows + me % kRows;   // the row whose scales this thread fetches
+                const int mine = (me / kRows * kGroups + group) * kRows + me % kRows;   // the row whose scales this thread fetches
                 const bool fetches = me < kChunks * kRows && mine < t.rows;
                 const float* from = p.x_scale + (int64_t)(t.row + mine) * groups;
                 float next = fetches ? ld_plain(from) : 0.0f;
                 bool ok = true;
                 for (int g = 0; g < groups; ++g) {
-                    float* here = scales + (g & 1) * 128;
-                    here[me] = next;
+                    float* here = scales + (g & 1) * kChunks * kRows;
+                    if (me < kChunks * kRows) here[me] = next;
                     if (fetches && g + 1 < groups) next = ld_plain(from + g + 1);
                     ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
                     ok = !group_or(1 + group, 128, !ok);   // (also: all scales are there)
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * kHalves * p.most;
+                    const bool done = g == groups - 1;
 #pragma unroll
-                    for (int i0 = 0; i0 < kChunks; i0 += 4) {   // (a batch's columns are there whether rows use them or not)
-                        const int c = (2 * i0 + group) * kRows;
-                        if (c >= t.rows) break;
-                        float v[4][16];
-                        if constexpr (CG == 1) tmem_ld_pieces(d + c, d + p.most + c, v);
-                        else tmem_ld_pieces(d + c, v);
+                    for (int i0 = 0; i0 < kChunks; i0 += 2) {   // (two pieces' columns are there whether rows use them or not)
+                        const int c = (kGroups * i0 + group) * kRows;
+                        float v[2][16];
+                        if (c < t.rows) {
+                            if constexpr (CG == 1) tmem_ld_pieces(d + c, d + p.most + c, v);
+                            else tmem_ld_pieces(d + c, v);
+                        }
+                        if (i0 + 2 == kChunks && !done) {   // all of them have been read: the products may go on
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) {
+                                if constexpr (CG == 1) mbar_arrive(&sh.acc_empty[acc]);
+                                else mbar_arrive_pair_relaxed(first_of_pair(&sh.acc_empty[acc]));
+                            }
+                        }
+                        if (c >= t.rows) continue;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
                             for (int j = 0; j < kRows; j += 8) {
                                 const float2 s = *reinterpret_cast<const float2*>(here + (i0 + i) * kRows + j + 2 * (lane & 3));
@@ -253,24 +284,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                                 }
                             }
                     }
-                    if (g == groups - 1) {   // the whole sums take the place of the last group's
+                    if (done) {   // the whole sums take the place of the last group's
 #pragma unroll
                         for (int i = 0; i < kChunks; ++i) {
-                            const int c = (2 * i + group) * kRows;
+                            const int c = (kGroups * i + group) * kRows;
                             if (c < t.rows) {
                                 if constexpr (CG == 1) tmem_st_piece(d + c, d + p.most + c, sum[i]);
                                 else tmem_st_piece(d + c, sum[i]);
                             }
                         }
-                        break;
-                    }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 1) mbar_arrive(&sh.acc_empty[acc]);
-                        else mbar_arrive_pair_relaxed(first_of_pair(&sh.acc_empty[acc]));
-                    }
-                    if (++acc == p.accs) {
+                    } else if (++acc == p.accs) {
                         acc = 0;
                         acc_phase ^= 1;
                     }
@@ -328,7 +351,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                 // pair: eight lanes gate, the next eight lanes up of the same features, so that a lane finishes every second row
                 constexpr int kRows = gated(MODE) && CG == 1 ? 8 : 16;
                 constexpr int kWidth = gated(MODE) && CG == 2 ? 64 : 128, kPitch = kWidth == 64 ? kNarrow : kWide;
-                constexpr int kTile = kRows * kPitch, kVecs = kWidth / 8, kPasses = kRows * kVecs / 128;
+                constexpr int kVecs = kWidth / 8, kPasses = kRows * kVecs / 128;
                 const int me = threadIdx.x - kFirstResult * 32 - group * 128;   // thread of the column group
                 for (int h = 0; h < (gated(MODE) ? 1 : kHalves); ++h) {
                     const int f0 = t.f0 + (gated(MODE) ? rank * kWidth : (h + rank) * 128);
@@ -359,9 +382,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                             bias = __uint_as_float((uint32_t)ld_plain(p.bias + (int64_t)t.e * p.F + f0 + col) << 16);
                         if (p.residual) fetch(group * kRows);
                     }
-                    for (int c = group * kRows; c < t.rows; c += 2 * kRows) {
-                        const bool last = c + 2 * kRows >= t.rows && (gated(MODE) || h == kHalves - 1 || f0 + 128 >= p.F);
-                        uint8_t* tile = tiles + (p.pre ? 0 : flip * kTile);
+                    for (int c = group * kRows; c < t.rows; c += kGroups * kRows) {
+                        const bool last = c + kGroups * kRows >= t.rows && (gated(MODE) || h == kHalves - 1 || f0 + 128 >= p.F);
+                        uint8_t* tile = tiles + flip * kTile;
                         float v[16];
                         if constexpr (gated(MODE) && CG == 1) tmem_ld8x2(d + c, d + p.most + c, v, v + 8);
                         else tmem_ld16(d + h * p.most + c, v);
@@ -412,7 +435,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
 #pragma unroll
                                     for (int i = 0; i < kPasses; ++i)
                                         *reinterpret_cast<uint4*>(tile + (vec_row + i * (128 / kVecs)) * kPitch + me % kVecs * 16) = ahead[i];
-                                    if (c + 2 * kRows < t.rows) fetch(c + 2 * kRows);
+                                    if (c + kGroups * kRows < t.rows) fetch(c + kGroups * kRows);
                                     group_sync(1 + group, 128);
 #pragma unroll
                                     for (int i = 0; i < 16; ++i)
@@ -427,9 +450,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
                         if (p.pre) {
                             put_out(p.pre, gated(MODE) ? 2 * p.F : p.F, tile + kTile, c);
                             if (gated(MODE)) put_out(p.pre + p.F, 2 * p.F, tile + 2 * kTile, c);
-                            group_sync(1 + group, 128);
                         }
-                        flip ^= 1;   // (the other tile's readers have met at a barrier since)
+                        // (with two tiles in turn the other one's readers have met at a barrier since)
+                        if (p.pre || p.tiles == 1) group_sync(1 + group, 128);
+                        else flip ^= 1;
                     }
                 }
             }
@@ -441,161 +465,181 @@ __global__ void __launch_bounds__(kGemmThreads, 1) expert_kernel(const __grid_co
         }
         if constexpr (MODE == kWeightsGrad) bulk_wait_all<0>();
     } else {
-    if constexpr (kScaled) registers_down<40>();
+    if constexpr (kSplits) registers_down<kFewRegisters>();
+    // The loads and the products are each one thread's loop: with the whole warp in it (votes and elections in every step) a product's
+    // step took 60 cycles longer, of 512.
+    const bool lead = elect_one();
+    const uint32_t ring0 = smem_u32(ring);
     if (warp == 0) {
         // ------------------------------------------------------------------ loads
         int s = 0, used = 0, ends = 0;
         unsigned phase = 0;
         bool ok = true;
+        auto next_stage = [&] {
+            ++used;
+            if (++s == p.stages) {
+                s = 0;
+                phase ^= 1;
+            }
+        };
         for (int id = unit; ok && walk.find(id, t); id += units) {
             const int K = MODE == kWeightsGrad ? t.rows : p.K;
-            const int steps = (K + kStepK - 1) / kStepK;
             const bool two = kHalves == 2 && (gated(MODE) || t.f0 + 128 < p.F);
             const int f0 = t.f0 + rank * (gated(MODE) ? 64 : 128), fb0 = t.fb0 + rank * 128;
             // (in a pair each CTA brings one half of the rows, or of x's features)
             const int mine = CG == 1 ? t.rows : (t.rows + 31) / 32 * 16, row0 = t.row + rank * mine;
-            // (boxes of 64 and of 16 rows: a copy costs the loading warp some 55 cycles, eight copies of 16 rows nearly the whole step)
+            // (boxes of 64 and of 16 rows: a copy costs the loading thread some 55 cycles, eight copies of 16 rows nearly the whole step)
             const int small = MODE == kWeightsGrad ? 0 : (mine + 15) / 16 % 4, large = MODE == kWeightsGrad ? 4 / CG : (mine + 15) / 64;
             const unsigned bytes = (two ? 2 : 1) * kHalfBytes + large * 8192 + small * 2048;
-            const int passes = MODE == kWeightsGrad ? p.planes : 1;
-            for (int k = 0, plane = 0; k < steps; k += plane == passes - 1, plane = plane == passes - 1 ? 0 : plane + 1) {
-                ok = warp_wait<CG>(&sh.empty[s], phase ^ 1, &sh, p.status);
-                if (!ok) break;
-                if (elect_one()) {
-                    const uint32_t a = smem_u32(ring + (size_t)s * p.stage_bytes), b = a + kHalves * kHalfBytes;
-                    const int k0 = k * kStepK;
-                    uint32_t bar = CG == 1 ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
-                    if (kMends && K - k0 < kStepK) {   // each CTA counts its own last rows, which have to be mended
-                        uint64_t* end = &sh.ends[ends % kMaxRing];
-                        bar = smem_u32(end);
-                        mbar_arrive_expect_tx(end, bytes);
-                    } else if (rank == 0) {
-                        mbar_arrive_expect_tx(&sh.full[s], CG * bytes);
+            if (lead) {
+                for (int plane = 0; ok && plane < (MODE == kWeightsGrad ? p.planes : 1); ++plane)
+                    for (int k0 = 0; k0 < K; k0 += kStepK) {
+                        ok = thread_wait<CG>(&sh.empty[s], phase ^ 1, &sh, p.status);
+                        if (!ok) break;
+                        const uint32_t a = ring0 + s * p.stage_bytes, b = a + kHalves * kHalfBytes;
+                        uint32_t bar = CG == 1 ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
+                        if (kMends && K - k0 < kStepK) {   // each CTA counts its own last rows, which have to be mended
+                            uint64_t* end = &sh.ends[ends++ % kMaxRing];
+                            bar = smem_u32(end);
+                            mbar_arrive_expect_tx(end, bytes);
+                        } else if (rank == 0) {
+                            mbar_arrive_expect_tx(&sh.full[s], CG * bytes);
+                        }
+                        if constexpr (gated(MODE) && CG == 1) {
+                            tile_load<CG>(a, &map_a, k0, f0, 2 * t.e, bar);
+                            tile_load<CG>(a + kHalfBytes, &map_a, k0, f0, 2 * t.e + 1, bar);
+                        } else if constexpr (gated(MODE)) {
+                            tile_load5_pair(a, &map_a, k0, 0, 0, f0 / 8, t.e, bar);
+                        } else if constexpr (MODE == kLinear) {
+                            tile_load<CG>(a, &map_a, k0, f0, t.e, bar);
+                            if (two) tile_load<CG>(a + kHalfBytes, &map_a, k0, f0 + 128, t.e, bar);
+                        } else {
+                            const int y = MODE == kRowsGrad ? k0 : t.row + k0, z = MODE == kRowsGrad ? t.e : 0;
+                            tile_load<CG>(a, &map_a, f0, y, z, bar);
+                            tile_load<CG>(a + 8192, &map_a, f0 + 64, y, z, bar);
+                            if (two) {
+                                tile_load<CG>(a + 16384, &map_a, f0 + 128, y, z, bar);
+                                tile_load<CG>(a + 24576, &map_a, f0 + 192, y, z, bar);
+                            }
+                        }
+                        if constexpr (MODE == kWeightsGrad) {
+#pragma unroll
+                            for (int j = 0; j < 4 / CG; ++j) tile_load<CG>(b + j * 8192, &map_b, fb0 + 64 * j, t.row + k0, plane, bar);
+                        } else {
+                            for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, k0, row0 + j * 64, 0, bar);
+                            for (int j = 0; j < small; ++j)
+                                tile_load<CG>(b + large * 8192 + j * 2048, &map_c, k0, row0 + large * 64 + j * 16, 0, bar);
+                        }
+                        next_stage();
                     }
-                    if constexpr (gated(MODE) && CG == 1) {
-                        tile_load<CG>(a, &map_a, k0, f0, 2 * t.e, bar);
-                        tile_load<CG>(a + kHalfBytes, &map_a, k0, f0, 2 * t.e + 1, bar);
-                    } else if constexpr (gated(MODE)) {
-                        tile_load5_pair(a, &map_a, k0, 0, 0, f0 / 8, t.e, bar);
-                    } else if constexpr (MODE == kLinear) {
-                        tile_load<CG>(a, &map_a, k0, f0, t.e, bar);
-                        if (two) tile_load<CG>(a + kHalfBytes, &map_a, k0, f0 + 128, t.e, bar);
-                    } else {
-                        const int y = MODE == kRowsGrad ? k0 : t.row + k0, z = MODE == kRowsGrad ? t.e : 0;
-                        for (int j = 0; j < (two ? 4 : 2); ++j) tile_load<CG>(a + j * 8192, &map_a, f0 + 64 * j, y, z, bar);
-                    }
-                    if constexpr (MODE == kWeightsGrad)
-                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, fb0 + 64 * j, t.row + k0, plane, bar);
-                    else {
-                        for (int j = 0; j < large; ++j) tile_load<CG>(b + j * 8192, &map_b, k0, row0 + j * 64, 0, bar);
-                        for (int j = 0; j < small; ++j)
-                            tile_load<CG>(b + large * 8192 + j * 2048, &map_c, k0, row0 + large * 64 + j * 16, 0, bar);
-                    }
-                }
-                __syncwarp();
-                ends += kMends && K - k * kStepK < kStepK;
-                ++used;
-                if (++s == p.stages) {
-                    s = 0;
-                    phase ^= 1;
-                }
             }
+            ok = __all_sync(0xffffffffu, ok);
         }
-        if (CG == 2 && ok)   // the products' last arrivals come to this CTA's barriers: it may not leave before them
-            for (int i = 0; ok && i < p.stages && i < used; ++i) {
-                s = s ? s - 1 : p.stages - 1;
-                if (s == p.stages - 1) phase ^= 1;
-                ok = warp_wait<CG>(&sh.empty[s], phase, &sh, p.status);
-            }
-        else if (!ok) {
-            // nothing may still be on its way into shared memory when the CTA leaves: the last copy of every stage (a pair leaves
-            // together, and the first CTA's barriers count for both)
-            for (int i = 0; rank == 0 && i < p.stages && i < used; ++i) {
-                s = s ? s - 1 : p.stages - 1;
-                if (s == p.stages - 1) phase ^= 1;
-                mbar_wait(&sh.full[s], phase, nullptr);
-            }
+        if (lead) {
+            if (CG == 2 && ok)   // the products' last arrivals come to this CTA's barriers: it may not leave before them
+                for (int i = 0; ok && i < p.stages && i < used; ++i) {
+                    s = s ? s - 1 : p.stages - 1;
+                    if (s == p.stages - 1) phase ^= 1;
+                    ok = thread_wait<CG>(&sh.empty[s], phase, &sh, p.status);
+                }
+            else if (!ok && rank == 0)
+                // nothing may still be on its way into shared memory when the CTA leaves: the last copy of every stage (a pair leaves
+                // together, and the first CTA's barriers count for both)
+                for (int i = 0; i < p.stages && i < used; ++i) {
+                    s = s ? s - 1 : p.stages - 1;
+                    if (s == p.stages - 1) phase ^= 1;
+                    mbar_wait(&sh.full[s], phase, nullptr);
+                }
         }
+        __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------------------------ products
         int s = 0, acc = 0;
         unsigned phase = 0, acc_phase = 0;
         bool ok = true;
+        // (the first stage's operands; the address is the low end of a descriptor, and all of shared memory fits there)
+        const uint64_t a0 = kAcross ? operand(ring0, 8192, 1024) : operand(ring0, 16, 1024);
+        const uint64_t b0 = MODE == kWeightsGrad ? operand(ring0 + kHalves * kHalfBytes, 8192, 1024) : operand(ring0 + kHalves * kHalfBytes, 16, 1024);
+        constexpr int kPartA = (kAcross ? 2048 : 32) >> 4, kPartB = (MODE == kWeightsGrad ? 2048 : 32) >> 4;   // 16 of the contraction
         for (int id = unit; rank == 0 && ok && walk.find(id, t); id += units) {
             const int K = MODE == kWeightsGrad ? t.rows : p.K;
-            const int steps = (K + kStepK - 1) / kStepK;
-            if (steps == 0) continue;
             const bool two = kHalves == 2 && (gated(MODE) || t.f0 + 128 < p.F);
             const int n = MODE == kWeightsGrad ? 256 : (t.rows + 16 * CG - 1) / (16 * CG) * (16 * CG);
             const uint32_t idesc = instruction(128 * CG, n, kAcross, MODE == kWeightsGrad);
-            uint32_t d = 0;
-            const int passes = MODE == kWeightsGrad ? p.planes : 1;
-            for (int k = 0, plane = 0; k < steps; k += plane == passes - 1, plane = plane == passes - 1 ? 0 : plane + 1) {
-                // (rows with scales: every group of 128 channels is a sum of its own, two steps)
-                const bool opens = kScaled ? k % 2 == 0 : k + plane == 0, closes = kScaled ? k % 2 != 0 : k == steps - 1 && plane == passes - 1;
-                if (opens) {
-                    ok = warp_wait<CG>(&sh.acc_empty[acc], acc_phase ^ 1, &sh, p.status);
-                    if (!ok) break;
+            if (lead && K > 0) {
+                uint32_t d = 0;
+                bool add = false;
+                // rows with scales: every group of 128 channels is a sum of its own, two steps
+                auto open = [&] {
+                    ok = thread_wait<CG>(&sh.acc_empty[acc], acc_phase ^ 1, &sh, p.status);
                     tc_fence_after();
                     d = tmem + acc * kHalves * p.most;
-                }
-                ok = warp_wait<CG>(&sh.full[s], phase, &sh, p.status);
-                if (!ok) break;
-                uint8_t* stage = ring + (size_t)s * p.stage_bytes;
-                const int left = K - k * kStepK;
-                if constexpr (MODE == kWeightsGrad && CG == 1)
-                    if (left < kStepK) clear_rows(stage, kHalves * 2 + 4, left, lane);
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint32_t a = smem_u32(stage), b = a + kHalves * kHalfBytes;
-                    const int parts = left < kStepK ? (left + 15) / 16 : 4;
-                    for (int j = 0; j < parts; ++j) {
-                        const uint64_t da = kAcross ? operand(a + j * 2048, 8192, 1024) : operand(a + j * 32, 16, 1024);
-                        const uint64_t db = MODE == kWeightsGrad ? operand(b + j * 2048, 8192, 1024) : operand(b + j * 32, 16, 1024);
-                        const bool add = !opens || j != 0;
-                        mma_f16<CG>(d, da, db, idesc, add);
-                        if (two) mma_f16<CG>(d + p.most, da + (kHalfBytes >> 4), db, idesc, add);
+                    add = false;
+                };
+                auto close = [&] {
+                    mma_commit<CG>(&sh.acc_full[acc]);
+                    if (++acc == p.accs) {
+                        acc = 0;
+                        acc_phase ^= 1;
                     }
-                    mma_commit<CG>(&sh.empty[s]);
-                    if (closes) mma_commit<CG>(&sh.acc_full[acc]);
-                }
-                __syncwarp();
-                if (++s == p.stages) {
-                    s = 0;
-                    phase ^= 1;
-                }
-                if (closes && ++acc == p.accs) {
-                    acc = 0;
-                    acc_phase ^= 1;
-                }
+                };
+                auto part = [&](uint64_t da, uint64_t db) {
+                    mma_f16<CG>(d, da, db, idesc, add);
+                    if (two) mma_f16<CG>(d + p.most, da + (kHalfBytes >> 4), db, idesc, add);
+                    add = true;
+                };
+                if (!kScaled) open();
+                for (int plane = 0; ok && plane < (MODE == kWeightsGrad ? p.planes : 1); ++plane)
+                    for (int left = K; left > 0; left -= kStepK) {
+                        if (kScaled && (left & 64) == 0) open();   // (the contraction is a multiple of 128)
+                        if (kScaled && !ok) break;
+                        ok = thread_wait<CG>(&sh.full[s], phase, &sh, p.status);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t da = a0 + (uint32_t)(s * p.stage_bytes >> 4), db = b0 + (uint32_t)(s * p.stage_bytes >> 4);
+                        if (left >= kStepK) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) part(da + j * kPartA, db + j * kPartB);
+                        } else {
+                            for (int j = 0; j * 16 < left; ++j) part(da + j * kPartA, db + j * kPartB);
+                        }
+                        mma_commit<CG>(&sh.empty[s]);
+                        if (kScaled && (left & 64) != 0) close();
+                        if (++s == p.stages) {
+                            s = 0;
+                            phase ^= 1;
+                        }
+                    }
+                if (!kScaled && ok) close();
             }
+            ok = __all_sync(0xffffffffu, ok);
         }
         if (!ok) {   // no product may still be running when the tensor memory is given back
-            if (elect_one()) mma_commit<CG>(&sh.drained);
+            if (lead) mma_commit<CG>(&sh.drained);
             __syncwarp();
             mbar_wait(&sh.drained, 0, nullptr);
         }
     } else if (kMends && warp == 2) {
         // ------------------------------------------------------------------ last rows of a segment in the weights' gradient
-        // Both CTAs clear what is behind them in their own operands; the second tells the first, and the first completes the stage
-        // that its products wait for.  (Done for every step, the arrival at the other CTA alone took more than twice a step's time.)
+        // Each CTA clears what is behind them in its own operands; of a pair the second tells the first, and the first completes the
+        // stage that its products wait for.  (Done for every step, the arrival at the other CTA alone took more than twice a step's time.)
         int s = 0, ends = 0;
         bool ok = true;
         for (int id = unit; ok && walk.find(id, t); id += units) {
-            s += t.rows / kStepK * p.planes;
             const int left = t.rows % kStepK;
-            for (int plane = 0; left && plane < p.planes; ++plane, ++s, ++ends) {
-                const int at = s % p.stages, end = ends % kMaxRing;
-                const unsigned phase = ends / kMaxRing & 1;
+            for (int plane = 0; ok && plane < p.planes; ++plane) {
+                s += t.rows / kStepK;
+                if (!left) continue;
+                const int at = s++ % p.stages, end = ends % kMaxRing;
+                const unsigned phase = ends++ / kMaxRing & 1;
                 ok = warp_wait<CG>(&sh.ends[end], phase, &sh, p.status);
                 if (!ok) break;
-                clear_rows(ring + (size_t)at * p.stage_bytes, 4, left, lane);
-                if (rank == 0) {
-                    ok = warp_wait<CG>(&sh.cleared[end], phase, &sh, p.status);
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive(&sh.full[at]);
-                } else if (lane == 0) {
-                    mbar_arrive_pair(first_of_pair(&sh.cleared[end]));
+                clear_rows(ring + (size_t)at * p.stage_bytes, kHalves * 2 + 4 / CG, left, lane);
+                if (CG == 2 && rank == 0) ok = warp_wait<CG>(&sh.cleared[end], phase, &sh, p.status);
+                if (!ok) break;
+                if (lane == 0) {
+                    if (rank == 0) mbar_arrive(&sh.full[at]);
+                    else mbar_arrive_pair(first_of_pair(&sh.cleared[end]));
                 }
             }
             s %= p.stages;
@@ -852,7 +896,9 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     constexpr int kHalves = CG == 1 ? 2 : 1;
     p.stage_bytes = kHalves * kHalfBytes + p.most / CG * 128;
     p.accs = 2 * kHalves * p.most <= kColumns ? 2 : 1;
-    const int tiles = out_bytes(MODE);
+    // a tile of results per column group, and one for each array of saved products (the gated block in pairs has room for two in turn)
+    p.tiles = p.pre ? (gated(MODE) ? 3 : 2) : gated(MODE) ? 2 : 1;
+    const int tiles = result_groups(MODE) * (MODE == kWeightsGrad ? 1 : p.tiles) * tile_bytes(MODE, CG);
     const int room = dev.smem - 1024 - (int)sizeof(Shared) - tiles;
     p.stages = room / p.stage_bytes;
     if (p.stages > kMaxRing) p.stages = kMaxRing;
@@ -861,7 +907,7 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     static std::atomic<int> granted[kAttrDevices];
     e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, CG>), smem, granted);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, kGemmThreads, (size_t)smem, st, false, CG, a, b, c, p);
+    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE), (size_t)smem, st, false, CG, a, b, c, p);
 }
 
 // The segments of a call are not known to the host, their capacity is.

@@ -142,67 +142,44 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float* v) {
 // one, as v[0], v[1] and v[2], v[3].  So what goes by columns (here: the rows' scales) is needed for two of eight columns
 // per thread.  One "piece" is 32 lanes x 16 columns, 16 values: two halves of lanes, two groups of columns each; or, `pairs`, 8
 // columns at two addresses.
-// Four pieces, 32 columns apart; complete on return.
+// Two pieces, 32 columns apart; complete on return.
 __device__ __forceinline__ void tmem_ld_pieces(uint32_t addr, float (*v)[16]) {
-    uint32_t r[64];
+    uint32_t r[32];
     asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%64];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%65];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%16, %17, %18, %19, %20, %21, %22, %23}, [%66];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%24, %25, %26, %27, %28, %29, %30, %31}, [%67];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%32, %33, %34, %35, %36, %37, %38, %39}, [%68];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%40, %41, %42, %43, %44, %45, %46, %47}, [%69];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%48, %49, %50, %51, %52, %53, %54, %55}, [%70];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%56, %57, %58, %59, %60, %61, %62, %63}, [%71];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%32];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%33];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%16, %17, %18, %19, %20, %21, %22, %23}, [%34];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%24, %25, %26, %27, %28, %29, %30, %31}, [%35];\n"
         "tcgen05.wait::ld.sync.aligned;"
         : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]), "=&r"(r[7]), "=&r"(r[8]),
           "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]), "=&r"(r[14]), "=&r"(r[15]), "=&r"(r[16]),
           "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]), "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23]), "=&r"(r[24]),
-          "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31]), "=&r"(r[32]),
-          "=&r"(r[33]), "=&r"(r[34]), "=&r"(r[35]), "=&r"(r[36]), "=&r"(r[37]), "=&r"(r[38]), "=&r"(r[39]), "=&r"(r[40]),
-          "=&r"(r[41]), "=&r"(r[42]), "=&r"(r[43]), "=&r"(r[44]), "=&r"(r[45]), "=&r"(r[46]), "=&r"(r[47]), "=&r"(r[48]),
-          "=&r"(r[49]), "=&r"(r[50]), "=&r"(r[51]), "=&r"(r[52]), "=&r"(r[53]), "=&r"(r[54]), "=&r"(r[55]), "=&r"(r[56]),
-          "=&r"(r[57]), "=&r"(r[58]), "=&r"(r[59]), "=&r"(r[60]), "=&r"(r[61]), "=&r"(r[62]), "=&r"(r[63])
-        : "r"(addr), "r"(addr + (16u << 16)), "r"(addr + 32), "r"(addr + 32 + (16u << 16)), "r"(addr + 64),
-          "r"(addr + 64 + (16u << 16)), "r"(addr + 96), "r"(addr + 96 + (16u << 16)) : "memory");
+          "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31])
+        : "r"(addr), "r"(addr + (16u << 16)), "r"(addr + 32), "r"(addr + 32 + (16u << 16)) : "memory");
 #pragma unroll
-    for (int i = 0; i < 64; ++i) v[i / 16][i % 16] = __uint_as_float(r[i]);
+    for (int i = 0; i < 32; ++i) v[i / 16][i % 16] = __uint_as_float(r[i]);
 }
-// Four pieces of 8 columns, 16 apart, at each of two addresses.
+// Two pieces of 8 columns, 16 apart, at each of two addresses.
 __device__ __forceinline__ void tmem_ld_pieces(uint32_t addr, uint32_t addr2, float (*v)[16]) {
-    uint32_t r[64];
+    uint32_t r[32];
     asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%64];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%4, %5, %6, %7}, [%65];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%8, %9, %10, %11}, [%66];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%12, %13, %14, %15}, [%67];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%16, %17, %18, %19}, [%68];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%20, %21, %22, %23}, [%69];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%24, %25, %26, %27}, [%70];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%28, %29, %30, %31}, [%71];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%32, %33, %34, %35}, [%72];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%36, %37, %38, %39}, [%73];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%40, %41, %42, %43}, [%74];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%44, %45, %46, %47}, [%75];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%48, %49, %50, %51}, [%76];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%52, %53, %54, %55}, [%77];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%56, %57, %58, %59}, [%78];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%60, %61, %62, %63}, [%79];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%32];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%4, %5, %6, %7}, [%33];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%8, %9, %10, %11}, [%34];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%12, %13, %14, %15}, [%35];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%16, %17, %18, %19}, [%36];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%20, %21, %22, %23}, [%37];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%24, %25, %26, %27}, [%38];\n"
+        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%28, %29, %30, %31}, [%39];\n"
         "tcgen05.wait::ld.sync.aligned;"
         : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]), "=&r"(r[7]), "=&r"(r[8]),
           "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]), "=&r"(r[14]), "=&r"(r[15]), "=&r"(r[16]),
           "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]), "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23]), "=&r"(r[24]),
-          "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31]), "=&r"(r[32]),
-          "=&r"(r[33]), "=&r"(r[34]), "=&r"(r[35]), "=&r"(r[36]), "=&r"(r[37]), "=&r"(r[38]), "=&r"(r[39]), "=&r"(r[40]),
-          "=&r"(r[41]), "=&r"(r[42]), "=&r"(r[43]), "=&r"(r[44]), "=&r"(r[45]), "=&r"(r[46]), "=&r"(r[47]), "=&r"(r[48]),
-          "=&r"(r[49]), "=&r"(r[50]), "=&r"(r[51]), "=&r"(r[52]), "=&r"(r[53]), "=&r"(r[54]), "=&r"(r[55]), "=&r"(r[56]),
-          "=&r"(r[57]), "=&r"(r[58]), "=&r"(r[59]), "=&r"(r[60]), "=&r"(r[61]), "=&r"(r[62]), "=&r"(r[63])
-        : "r"(addr + 0), "r"(addr + 0 + (16u << 16)), "r"(addr2 + 0), "r"(addr2 + 0 + (16u << 16)),
-          "r"(addr + 16), "r"(addr + 16 + (16u << 16)), "r"(addr2 + 16), "r"(addr2 + 16 + (16u << 16)),
-          "r"(addr + 32), "r"(addr + 32 + (16u << 16)), "r"(addr2 + 32), "r"(addr2 + 32 + (16u << 16)),
-          "r"(addr + 48), "r"(addr + 48 + (16u << 16)), "r"(addr2 + 48), "r"(addr2 + 48 + (16u << 16)) : "memory");
+          "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31])
+        : "r"(addr), "r"(addr + (16u << 16)), "r"(addr2), "r"(addr2 + (16u << 16)), "r"(addr + 16), "r"(addr + 16 + (16u << 16)),
+          "r"(addr2 + 16), "r"(addr2 + 16 + (16u << 16)) : "memory");
 #pragma unroll
-    for (int i = 0; i < 64; ++i) v[i / 16][i % 16] = __uint_as_float(r[i]);
+    for (int i = 0; i < 32; ++i) v[i / 16][i % 16] = __uint_as_float(r[i]);
 }
 // One piece the other way; complete on return.
 __device__ __forceinline__ void tmem_st_piece(uint32_t addr, const float* v) {
