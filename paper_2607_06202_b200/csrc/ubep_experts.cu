@@ -175,8 +175,8 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
     constexpr bool kMends = MODE == kWeightsGrad;
     constexpr bool kScaled = MODE == kGatedScaled;
     constexpr int kGroups = result_groups(MODE), kTile = tile_bytes(MODE, CG);
-    // Rows with scales keep a tile's sums in the result warps' registers, which get some of the others'.
-    constexpr bool kSplits = kScaled;
+    // Rows with scales, in pairs: a tile's sums are kept in the result warps' registers, which get some of the others'.
+    constexpr bool kRowsFirst = kScaled && CG == 2, kSplits = kRowsFirst;
     constexpr int kFewRegisters = 40, kManyRegisters = 232;   // 384 threads x 168 = 128 x 40 + 256 x 232
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
     uint8_t* results = ring + (size_t)p.stages * p.stage_bytes;
@@ -227,26 +227,78 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
         unsigned acc_phase = 0;
         for (int id = unit; walk.find(id, t); id += units) {
             const bool empty = MODE == kWeightsGrad && t.rows == 0;
-            if constexpr (kScaled) {
+            if constexpr (kRowsFirst) {
+                // Rows with scales, in a pair: the rows are the lanes of tensor memory, so that a row's scale is one register of the thread
+                // that adds up its sums -- as columns every sum would need another scale, and those loads alone took as long as the
+                // products.  (The rows are half a pair's tile, the columns sixteens of gate and up of eight features.)
+                const int half = (t.rows + 31) / 32 * 16, r = rank * half + quarter * 32 + lane, groups = p.K / 128;
+                const bool mine = quarter * 32 + lane < half && r < t.rows;
+                const int64_t row = t.row + r;
+                const float* from = p.x_scale + row * groups;
+                float sum[128];
+#pragma unroll
+                for (int i = 0; i < 128; ++i) sum[i] = 0.0f;
+                float next = mine ? ld_plain(from) : 0.0f;
+                bool ok = true;
+                for (int g = 0; g < groups; ++g) {
+                    const float2 scale = make_float2(next, next);
+                    if (mine && g + 1 < groups) next = ld_plain(from + g + 1);
+                    ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * 256 + group * 128;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float v[64];
+                        tmem_ld64(d + h * 64, v);
+                        if (h == 1) {   // all of them have been read: the products may go on
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_pair_relaxed(first_of_pair(&sh.acc_empty[acc]));
+                        }
+#pragma unroll
+                        for (int i = 0; i < 64; i += 2) fma_two(sum + h * 64 + i, v + i, scale);
+                    }
+                    if (++acc == p.accs) {
+                        acc = 0;
+                        acc_phase ^= 1;
+                    }
+                }
+                if (group_or(1 + group, 128, !ok)) break;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int f = t.f0 + group * 64 + i * 8;
+                    if (f >= p.F || !mine) continue;
+                    float *g = sum + i * 16, *u = g + 8;
+                    if (p.pre) {
+                        st_vec(p.pre + row * 2 * p.F + f, pack8(g));
+                        st_vec(p.pre + (row * 2 + 1) * p.F + f, pack8(u));
+                    }
+                    act_values<8>(g, p.act);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[j] *= u[j];
+                    st_vec(p.out + row * p.F + f, pack8(g));
+                }
+                continue;
+            } else if constexpr (kScaled) {
                 // Rows with scales: the sum over every 128 channels is multiplied with the row's scale of them and added up here, in
                 // 32 bits -- the e4m3 values are bf16 exactly, their products with the scales would be rounded once more.
-                constexpr int kRows = CG == 1 ? 8 : 16, kChunks = (CG == 1 ? 64 : 256) / kRows / kGroups;
-                float sum[kChunks][16];
+                float sum[4][16];
 #pragma unroll
-                for (int i = 0; i < kChunks; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) sum[i][j] = 0.0f;
                 group_sync(1 + group, 128);   // (the last tile's results have left the room)
                 float* scales = reinterpret_cast<float*>(tiles);
                 const int me = threadIdx.x - kFirstResult * 32 - group * 128, groups = p.K / 128;
-                const int mine = (me / kRows * kGroups + group) * kRows + me % kRows;   // the row whose scales this thread fetches
-                const bool fetches = me < kChunks * kRows && mine < t.rows;
+                const int mine = (me / 8 * 2 + group) * 8 + me % 8;   // the row whose scales this thread fetches
+                const bool fetches = me < 32 && mine < t.rows;
                 const float* from = p.x_scale + (int64_t)(t.row + mine) * groups;
                 float next = fetches ? ld_plain(from) : 0.0f;
                 bool ok = true;
                 for (int g = 0; g < groups; ++g) {
-                    float* here = scales + (g & 1) * kChunks * kRows;
-                    if (me < kChunks * kRows) here[me] = next;
+                    float* here = scales + (g & 1) * 32;
+                    if (me < 32) here[me] = next;
                     if (fetches && g + 1 < groups) next = ld_plain(from + g + 1);
                     ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
                     ok = !group_or(1 + group, 128, !ok);   // (also: all scales are there)
@@ -255,43 +307,28 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                     const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * kHalves * p.most;
                     const bool done = g == groups - 1;
 #pragma unroll
-                    for (int i0 = 0; i0 < kChunks; i0 += 2) {   // (two pieces' columns are there whether rows use them or not)
-                        const int c = (kGroups * i0 + group) * kRows;
+                    for (int i0 = 0; i0 < 4; i0 += 2) {   // (two pieces' columns are there whether rows use them or not)
+                        const int c = (2 * i0 + group) * 8;
                         float v[2][16];
-                        if (c < t.rows) {
-                            if constexpr (CG == 1) tmem_ld_pieces(d + c, d + p.most + c, v);
-                            else tmem_ld_pieces(d + c, v);
-                        }
-                        if (i0 + 2 == kChunks && !done) {   // all of them have been read: the products may go on
+                        if (c < t.rows) tmem_ld_pieces(d + c, d + p.most + c, v);
+                        if (i0 == 2 && !done) {   // all of them have been read: the products may go on
                             tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) {
-                                if constexpr (CG == 1) mbar_arrive(&sh.acc_empty[acc]);
-                                else mbar_arrive_pair_relaxed(first_of_pair(&sh.acc_empty[acc]));
-                            }
+                            if (lane == 0) mbar_arrive(&sh.acc_empty[acc]);
                         }
                         if (c >= t.rows) continue;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 s = *reinterpret_cast<const float2*>(here + (i0 + i) * 8 + 2 * (lane & 3));
 #pragma unroll
-                            for (int j = 0; j < kRows; j += 8) {
-                                const float2 s = *reinterpret_cast<const float2*>(here + (i0 + i) * kRows + j + 2 * (lane & 3));
-#pragma unroll
-                                for (int q = 0; q < (CG == 1 ? 16 : 8); q += 2) {
-                                    // (a pair's piece: halves of lanes, eight values each, of which four of these columns)
-                                    const int at = CG == 1 ? q : q / 4 * 8 + j / 2 + q % 4;
-                                    fma_two(sum[i0 + i] + at, v[i] + at, s);
-                                }
-                            }
+                            for (int q = 0; q < 16; q += 2) fma_two(sum[i0 + i] + q, v[i] + q, s);
+                        }
                     }
                     if (done) {   // the whole sums take the place of the last group's
 #pragma unroll
-                        for (int i = 0; i < kChunks; ++i) {
-                            const int c = (kGroups * i + group) * kRows;
-                            if (c < t.rows) {
-                                if constexpr (CG == 1) tmem_st_piece(d + c, d + p.most + c, sum[i]);
-                                else tmem_st_piece(d + c, sum[i]);
-                            }
+                        for (int i = 0; i < 4; ++i) {
+                            const int c = (2 * i + group) * 8;
+                            if (c < t.rows) tmem_st_piece(d + c, d + p.most + c, sum[i]);
                         }
                     } else if (++acc == p.accs) {
                         acc = 0;
@@ -564,7 +601,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
         for (int id = unit; rank == 0 && ok && walk.find(id, t); id += units) {
             const int K = MODE == kWeightsGrad ? t.rows : p.K;
             const bool two = kHalves == 2 && (gated(MODE) || t.f0 + 128 < p.F);
-            const int n = MODE == kWeightsGrad ? 256 : (t.rows + 16 * CG - 1) / (16 * CG) * (16 * CG);
+            const int n = MODE == kWeightsGrad || kRowsFirst ? 256 : (t.rows + 16 * CG - 1) / (16 * CG) * (16 * CG);
             const uint32_t idesc = instruction(128 * CG, n, kAcross, MODE == kWeightsGrad);
             if (lead && K > 0) {
                 uint32_t d = 0;
@@ -584,7 +621,8 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                     }
                 };
                 auto part = [&](uint64_t da, uint64_t db) {
-                    mma_f16<CG>(d, da, db, idesc, add);
+                    if (kRowsFirst) mma_f16<CG>(d, db, da, idesc, add);
+                    else mma_f16<CG>(d, da, db, idesc, add);
                     if (two) mma_f16<CG>(d + p.most, da + (kHalfBytes >> 4), db, idesc, add);
                     add = true;
                 };

@@ -138,27 +138,31 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float* v) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
+// 64 columns of the warp's 32 lanes; complete on return.
+__device__ __forceinline__ void tmem_ld64(uint32_t addr, float* v) {
+    uint32_t r[64];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+        "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, "
+        "%42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, "
+        "%62, %63"
+        "}, [%64];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]),
+          "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]),
+          "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]),
+          "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "r"(addr) : "memory");
+#pragma unroll
+    for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
+}
 // Tensor memory in the other order: of 16 lanes and 8 columns a thread holds lanes l / 4 and l / 4 + 8, columns 2 (l % 4) and the next
 // one, as v[0], v[1] and v[2], v[3].  So what goes by columns (here: the rows' scales) is needed for two of eight columns
-// per thread.  One "piece" is 32 lanes x 16 columns, 16 values: two halves of lanes, two groups of columns each; or, `pairs`, 8
-// columns at two addresses.
-// Two pieces, 32 columns apart; complete on return.
-__device__ __forceinline__ void tmem_ld_pieces(uint32_t addr, float (*v)[16]) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%32];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%33];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%16, %17, %18, %19, %20, %21, %22, %23}, [%34];\n"
-        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%24, %25, %26, %27, %28, %29, %30, %31}, [%35];\n"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]), "=&r"(r[7]), "=&r"(r[8]),
-          "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]), "=&r"(r[14]), "=&r"(r[15]), "=&r"(r[16]),
-          "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]), "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23]), "=&r"(r[24]),
-          "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31])
-        : "r"(addr), "r"(addr + (16u << 16)), "r"(addr + 32), "r"(addr + 32 + (16u << 16)) : "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i / 16][i % 16] = __uint_as_float(r[i]);
-}
+// per thread.  One "piece" is 32 lanes x 8 columns at two addresses, 16 values.
 // Two pieces of 8 columns, 16 apart, at each of two addresses.
 __device__ __forceinline__ void tmem_ld_pieces(uint32_t addr, uint32_t addr2, float (*v)[16]) {
     uint32_t r[32];
@@ -182,13 +186,6 @@ __device__ __forceinline__ void tmem_ld_pieces(uint32_t addr, uint32_t addr2, fl
     for (int i = 0; i < 32; ++i) v[i / 16][i % 16] = __uint_as_float(r[i]);
 }
 // One piece the other way; complete on return.
-__device__ __forceinline__ void tmem_st_piece(uint32_t addr, const float* v) {
-    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%2, %3, %4, %5, %6, %7, %8, %9};\n"
-                 "tcgen05.st.sync.aligned.16x256b.x2.b32 [%1], {%10, %11, %12, %13, %14, %15, %16, %17};\n"
-                 "tcgen05.wait::st.sync.aligned;"
-                 ::"r"(addr), "r"(addr + (16u << 16)), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]),
-                   "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]) : "memory");
-}
 __device__ __forceinline__ void tmem_st_piece(uint32_t addr, uint32_t addr2, const float* v) {
     asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%4, %5, %6, %7};\n"
                  "tcgen05.st.sync.aligned.16x256b.x1.b32 [%1], {%8, %9, %10, %11};\n"
