@@ -519,15 +519,17 @@ int ubep_expert_linear(const ubep_expert_rows_t *rows /*[host]*/, const void *x 
 /*
  * Its gradients, with dz = row_scale grad_y act'(pre): grad_x = dz W ([dev] bf16 [R, cap, K]), grad_w = dz^T x ([dev] bf16
  * [E, N, K]), grad_bias = column sums of dz ([dev] bf16 [E, N]), grad_row_scale = <grad_y, act(pre)> ([dev] fp32 [R, cap]; needs
- * row_scale); each may be NULL, and experts without rows get zeros.  (The residual's gradient is grad_y.)  pre and
- * grad_pre ([dev] bf16 [R, cap, N], room for dz rounded to bf16; may be pre itself unless grad_bias is
- * asked for) are needed with an activation or row_scale and not read without.  Up to four launches.
+ * row_scale, and N at most 16384); each may be NULL, and experts without rows get zeros.  (The residual's gradient is
+ * grad_y.)  pre and grad_pre ([dev] bf16 [R, cap, N], room for dz rounded to bf16; may be pre itself) are needed with an
+ * activation or row_scale and not touched without.  scratch [dev] fp32 [max(E, UBEP_EXPERT_PARTIALS), N] is needed
+ * for grad_bias: sums of slices of the experts' rows, which are joined in order.  Up to four launches.
  */
+#define UBEP_EXPERT_PARTIALS 1024
 int ubep_expert_linear_backward(const ubep_expert_rows_t *rows /*[host]*/, const void *x /*[dev]*/, const void *w /*[dev]*/,
                                 const void *pre /*[dev]*/, const float *row_scale /*[dev]*/, const void *grad_y /*[dev]*/,
                                 int32_t K, int32_t N, int act, void *grad_pre /*[dev]*/, void *grad_x /*[dev]*/,
                                 void *grad_w /*[dev]*/, void *grad_bias /*[dev]*/, float *grad_row_scale /*[dev]*/,
-                                void *cuda_stream);
+                                float *scratch /*[dev]*/, void *cuda_stream);
 
 /* Device address and shape (unused dims = 1) of one arena array; valid until destroy. */
 int ubep_view(ubep_buffer_t *buf, int which, void **dev_ptr /*[host]*/, int64_t shape[4] /*[host]*/);

@@ -141,7 +141,7 @@ def load() -> ctypes.CDLL:
     lib.ubep_expert_linear.restype = ctypes.c_int
     lib.ubep_expert_linear.argtypes = [rowsp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp]
     lib.ubep_expert_linear_backward.restype = ctypes.c_int
-    lib.ubep_expert_linear_backward.argtypes = [rowsp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp, vp, vp, vp]
+    lib.ubep_expert_linear_backward.argtypes = [rowsp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp, vp, vp, vp, vp]
     native = _load_native()
     native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                   (lib.ubep_dispatch, lib.ubep_combine, lib.ubep_get_dispatch_layout, lib.ubep_dispatch_sync,

@@ -66,6 +66,23 @@ __device__ __forceinline__ void act_both(float z, int act, float& value, float& 
     }
 }
 
+// Of eight at once, one branch for all of them.
+__device__ __forceinline__ void act_both8(const float* z, int act, float* value, float* slope) {
+    if (act == kActSilu) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) act_both(z[i], kActSilu, value[i], slope[i]);
+    } else if (act == kActGelu) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) act_both(z[i], kActGelu, value[i], slope[i]);
+    } else if (act == kActRelu) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) act_both(z[i], kActRelu, value[i], slope[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) act_both(z[i], kActNone, value[i], slope[i]);
+    }
+}
+
 __device__ __forceinline__ void unpack8(const uint4 in, float* f) {
     const uint32_t w[4] = {in.x, in.y, in.z, in.w};
 #pragma unroll

@@ -16,8 +16,8 @@ cudaError_t launch_expert_linear(const ubep_expert_rows_t& r, const void* x, con
                                  const void* residual, int K, int N, int act, void* y, void* pre, cudaStream_t st, int* launches);
 cudaError_t launch_expert_linear_backward(const ubep_expert_rows_t& r, const void* x, const void* w, const void* pre,
                                           const float* row_scale, const void* grad_y, int K, int N, int act, void* grad_pre,
-                                          void* grad_x, void* grad_w, void* grad_bias, float* grad_scale, cudaStream_t st,
-                                          int* launches);
+                                          void* grad_x, void* grad_w, void* grad_bias, float* grad_scale, float* scratch,
+                                          cudaStream_t st, int* launches);
 cudaError_t launch_route(const void* logits, int type, int T, int E, int k, int renormalize, int32_t* topk_idx, float* topk_w,
                          cudaStream_t st);
 cudaError_t launch_route_backward(const void* logits, int type, const int32_t* topk_idx, const float* grad_w, int T, int E, int k,

@@ -963,15 +963,17 @@ int ubep_expert_linear(const ubep_expert_rows_t* rows, const void* x, const void
 
 int ubep_expert_linear_backward(const ubep_expert_rows_t* rows, const void* x, const void* w, const void* pre, const float* row_scale,
                                 const void* grad_y, int32_t K, int32_t N, int act, void* grad_pre, void* grad_x, void* grad_w,
-                                void* grad_bias, float* grad_row_scale, void* cuda_stream) {
-    if (!expert_args(rows, K, N, act) || !arrays({grad_y}, {x, w, pre, row_scale, grad_pre, grad_x, grad_w, grad_bias, grad_row_scale}))
+                                void* grad_bias, float* grad_row_scale, float* scratch, void* cuda_stream) {
+    if (!expert_args(rows, K, N, act) ||
+        !arrays({grad_y}, {x, w, pre, row_scale, grad_pre, grad_x, grad_w, grad_bias, grad_row_scale, scratch}))
         return UBEP_ERR_ARG;
+    if ((grad_bias && !scratch) || (grad_row_scale && N > 16384)) return UBEP_ERR_ARG;
     if ((grad_x && !w) || (grad_w && !x) || (grad_row_scale && !row_scale)) return UBEP_ERR_ARG;
-    if ((act != UBEP_ACT_NONE || row_scale) && (!pre || !grad_pre || (grad_pre == pre && grad_bias))) return UBEP_ERR_ARG;
+    if ((act != UBEP_ACT_NONE || row_scale) && (!pre || !grad_pre)) return UBEP_ERR_ARG;
     if (!grad_x && !grad_w && !grad_bias && !grad_row_scale) return UBEP_ERR_ARG;
     return on_device(rows->device, [&](int* n) {
         return ubep::launch_expert_linear_backward(*rows, x, w, pre, row_scale, grad_y, K, N, act, grad_pre, grad_x, grad_w, grad_bias,
-                                                   grad_row_scale, static_cast<cudaStream_t>(cuda_stream), n);
+                                                   grad_row_scale, scratch, static_cast<cudaStream_t>(cuda_stream), n);
     });
 }
 

@@ -15,6 +15,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstdio>
 #include <exception>
@@ -588,10 +589,13 @@ PyObject* py_linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         Output gx(a[10], "grad_x", at, at::kBFloat16, {x.R, x.cap, x.width}, true), gw(a[11], "grad_w", at, at::kBFloat16, w.sizes(), true),
             gb(a[12], "grad_bias", at, at::kBFloat16, {(int64_t)r.num_experts, N}, false),
             gs(a[13], "grad_row_scale", at, at::kFloat, {x.R, x.cap}, false);
+        at::Tensor sums;
+        if (gb.ptr) sums = at.scratch({std::max<int64_t>(r.num_experts, UBEP_EXPERT_PARTIALS), N}, at::kFloat);
+        float* ps = gb.ptr ? sums.data_ptr<float>() : nullptr;
         const void *px = x.t.data_ptr(), *pw = w.data_ptr(), *py = gy.data_ptr();
         const int32_t K = narrow(x.width, "x"), Ni = narrow(N, "w");
         const int rc = without_gil([&] {
-            return f_linear_backward(&r, px, pw, pre, scale, py, K, Ni, act, gp, gx.ptr, gw.ptr, gb.ptr, static_cast<float*>(gs.ptr), at.stream);
+            return f_linear_backward(&r, px, pw, pre, scale, py, K, Ni, act, gp, gx.ptr, gw.ptr, gb.ptr, static_cast<float*>(gs.ptr), ps, at.stream);
         });
         if (rc != UBEP_OK) return PyLong_FromLong(rc);
         return Py_BuildValue("(NNNN)", gx.result(), gw.result(), gb.result(), gs.result());

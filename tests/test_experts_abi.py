@@ -64,9 +64,10 @@ def test_linear_arguments(lib):
 
 
 def test_linear_backward_arguments(lib):
-    def call(x=P, w=P, pre=P, scale=None, gy=P, K=64, N=64, act=1, gp=2 * P, gx=P, gw=P, gb=None, gs=None):
-        return lib.ubep_expert_linear_backward(_rows(), x, w, pre, scale, gy, K, N, act, gp, gx, gw, gb, gs, None)
-    for bad in (dict(gy=None), dict(pre=None), dict(gp=None), dict(gs=P), dict(w=None), dict(x=None), dict(gp=P, gb=P),
+    def call(x=P, w=P, pre=P, scale=None, gy=P, K=64, N=64, act=1, gp=2 * P, gx=P, gw=P, gb=None, gs=None, scratch=None):
+        return lib.ubep_expert_linear_backward(_rows(), x, w, pre, scale, gy, K, N, act, gp, gx, gw, gb, gs, scratch, None)
+    for bad in (dict(gy=None), dict(pre=None), dict(gp=None), dict(gs=P), dict(w=None), dict(x=None), dict(gb=P),
+                dict(gb=P, scratch=ODD), dict(scale=P, gs=P, N=16392),
                 dict(gx=None, gw=None), dict(gx=ODD), dict(scale=P, act=0, pre=None)):
         assert call(**bad) == B.UBEP_ERR_ARG, bad
 

@@ -328,6 +328,15 @@ def test_linear_backward(segments, K, N):
             gb[e] = d[r, a:b].sum(0)
             tb[e] = ((b - a + 4) * SUM * d[r, a:b].abs() + size[r, a:b]).sum(0)
         check_all("grad_bias", grad_b, gb, tb * (1 + HALF) + HALF * gb.abs())
+        if used:   # the gradients of pre in pre's own memory, and what no product needs by itself
+            own, alone = pre.clone(), R.filled(K)
+            got = B.expert_linear_backward(R.rows, x, w, grad, pre=own, row_scale=scale if use_scale else None, act=act, grad_x=alone,
+                                           grad_w=False, grad_pre=own, grad_bias=True)
+            assert torch.equal(alone, grad_x) and torch.equal(got[2], grad_b)
+            assert torch.equal(own[~R.mine].view(torch.int16), pre[~R.mine].view(torch.int16))
+        got = B.expert_linear_backward(R.rows, x, w, grad, pre=pre if used else None, row_scale=scale if use_scale else None, act=act,
+                                       grad_x=False, grad_w=False, grad_bias=True)
+        assert got[0] is None and got[1] is None and torch.equal(got[2], grad_b)
         if use_scale:
             gs = (dy * v).sum(-1)
             ts = ((N + 4) * SUM * (dy * v).abs() + (dy * (1 + z.abs())).abs() * 2.0 ** -18).sum(-1)
@@ -396,8 +405,7 @@ def test_refusals():
                  lambda: B.expert_linear(B.ExpertRows(R.rows.offset[:5], R.rows.count[:5]), x, w3[:5].contiguous()),   # 5 experts, 2 regions
                  lambda: B.expert_linear_backward(R.rows, x, w3, grad, act="silu"),                     # no pre
                  lambda: B.expert_linear_backward(R.rows, x, w3, grad, grad_row_scale=True),            # no row_scale
-                 lambda: B.expert_linear_backward(R.rows, x, w3, grad, grad_x=False, grad_w=False),     # nothing asked for
-                 lambda: B.expert_linear_backward(R.rows, x, w3, grad, pre=grad, act="silu", grad_pre=grad, grad_bias=True)):
+                 lambda: B.expert_linear_backward(R.rows, x, w3, grad, grad_x=False, grad_w=False)):    # nothing asked for
         with pytest.raises(B.UbepError) as e:
             call()
         assert e.value.code == B.UBEP_ERR_ARG
