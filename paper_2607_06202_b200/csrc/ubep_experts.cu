@@ -34,7 +34,7 @@ __host__ __device__ constexpr bool gated(int mode) { return mode == kGated || mo
 // A warpgroup with a loading warp, a multiplying warp and (weights' gradient in pairs) one that mends the last rows; the others turn
 // sums into results: in groups of four warps, which share the tile's columns.
 constexpr int kFirstResult = 4;
-__host__ __device__ constexpr int result_groups(int) { return 2; }
+__host__ __device__ constexpr int result_groups(int mode) { return mode == kLinear ? 4 : 2; }
 __host__ __device__ constexpr int gemm_threads(int mode) { return 32 * (kFirstResult + 4 * result_groups(mode)); }
 constexpr int kStepK = 64;               // of the contraction per stage: 128 bytes of bf16, the swizzle's width
 constexpr int kHalfBytes = 128 * 128;    // 128 features of one stage
@@ -57,6 +57,7 @@ struct Product {
     int most;        // rows per tile at most; columns of one accumulator
     int stages, stage_bytes, accs;
     int tiles;       // of results per column group
+    int span;        // features per tile: 128 per CTA, or 256 for a single one (gated block: 128 of each matrix, 64 in pairs)
     int act;
     uint16_t *out, *pre;
     const uint16_t *bias, *residual;
@@ -117,12 +118,11 @@ struct Walk {
     TileWalk w;
     const Product& p;
     int per_row_tile, fb_tiles;
-    static constexpr int kFeatures = gated(MODE) ? 128 : 256;
     static constexpr bool kEvery = MODE == kWeightsGrad;
     static constexpr int kUnit = 16 * CG;
     __device__ __forceinline__ explicit Walk(const Product& p_) : p(p_) {
         fb_tiles = kEvery ? (p.FB + 255) / 256 : 1;
-        per_row_tile = (p.F + kFeatures - 1) / kFeatures * fb_tiles;
+        per_row_tile = (p.F + p.span - 1) / p.span * fb_tiles;
         w.base = w.before = 0;
         w.load(p.seg, per_row_tile, p.most, kEvery);
     }
@@ -131,7 +131,7 @@ struct Walk {
         if (!w.find(p.seg, per_row_tile, p.most, kEvery, t, o.e, first, rows, place)) return false;
         if (kEvery) {
             // (neighbours share the tile of the first operand)
-            o.f0 = place / fb_tiles * kFeatures;
+            o.f0 = place / fb_tiles * p.span;
             o.fb0 = place % fb_tiles * 256;
             o.row = first;
             o.rows = rows;
@@ -140,7 +140,7 @@ struct Walk {
             const int n = row_tiles(rows, p.most);
             const int piece = ((rows + n - 1) / n + kUnit - 1) / kUnit * kUnit;
             const int i = place % n;
-            o.f0 = place / n * kFeatures;
+            o.f0 = place / n * p.span;
             o.fb0 = 0;
             o.row = first + i * piece;
             o.rows = min(piece, rows - i * piece);
@@ -161,6 +161,56 @@ __device__ __forceinline__ void clear_rows(uint8_t* stage, int blocks, int left,
 }
 
 __device__ __forceinline__ void put_bf16(uint8_t* at, float v) { *reinterpret_cast<__nv_bfloat16*>(at) = __float2bfloat16_rn(v); }
+__device__ __forceinline__ uint4 ld_vec(const uint16_t* p);
+// What the linear product's epilogue reads besides the sums, fetched two chunks of 16 rows ahead: the bias of the thread's features,
+// the rows' weights (lane l: row l of the chunk) and the thread's 16-byte pieces of the residual, rows and columns as they are
+// written out.
+template <bool USED, int HALVES, int GROUPS>
+struct Extras {
+    float bias[2], scale, scale1;
+    uint4 rows[2], rows1[2];
+    int h, c, start, vec, vec_row, lane;
+    __device__ __forceinline__ void fetch(const Product& p, const Tile& t, int rank, uint4* to, float& s) {
+        const int f = t.f0 + (h + rank) * 128 + vec;
+        const bool in = h < HALVES && (h == 0 || p.span == 256) && f < p.F;
+        if (p.residual) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = c + vec_row + i * 8;
+                to[i] = in && r < t.rows ? ld_vec(p.residual + (int64_t)(t.row + r) * p.F + f) : make_uint4(0, 0, 0, 0);
+            }
+        }
+        if (p.row_scale) s = lane < 16 && c + lane < t.rows ? ld_plain(p.row_scale + t.row + c + lane) : 0.0f;
+        c += GROUPS * 16;
+        if (c >= t.rows) {
+            c = start;
+            ++h;
+        }
+    }
+    __device__ __forceinline__ void begin(const Product& p, const Tile& t, int rank, int group, int lane_) {
+        if constexpr (!USED) return;
+        const int me = threadIdx.x - kFirstResult * 32 - group * 128;
+        lane = lane_;
+        h = 0;
+        c = start = group * 16;
+        vec = me % 16 * 8;
+        vec_row = me / 16;
+#pragma unroll
+        for (int i = 0; i < HALVES; ++i) {
+            const int f = t.f0 + (i + rank) * 128 + (me >> 5) % 4 * 32 + lane;
+            bias[i] = p.bias && f < p.F ? __uint_as_float((uint32_t)ld_plain(p.bias + (int64_t)t.e * p.F + f) << 16) : 0.0f;
+        }
+        fetch(p, t, rank, rows, scale);
+        fetch(p, t, rank, rows1, scale1);
+    }
+    __device__ __forceinline__ void next(const Product& p, const Tile& t, int rank) {
+        scale = scale1;
+        rows[0] = rows1[0];
+        rows[1] = rows1[1];
+        fetch(p, t, rank, rows1, scale1);
+    }
+};
+
 __device__ __forceinline__ uint4 ld_vec(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
@@ -176,8 +226,9 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
     constexpr bool kScaled = MODE == kGatedScaled;
     constexpr int kGroups = result_groups(MODE), kTile = tile_bytes(MODE, CG);
     // Rows with scales, in pairs: a tile's sums are kept in the result warps' registers, which get some of the others'.
-    constexpr bool kRowsFirst = kScaled && CG == 2, kSplits = kRowsFirst;
-    constexpr int kFewRegisters = 40, kManyRegisters = 232;   // 384 threads x 168 = 128 x 40 + 256 x 232
+    constexpr bool kRowsFirst = kScaled && CG == 2, kSplits = kRowsFirst || kGroups == 4;
+    // 384 threads x 168 = 128 x 40 + 256 x 232; 640 threads x 96 = 61440, 128 x 48 + 512 x 104 = 59392
+    constexpr int kFewRegisters = kGroups == 2 ? 40 : 48, kManyRegisters = kGroups == 2 ? 232 : 104;
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
     uint8_t* results = ring + (size_t)p.stages * p.stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -215,6 +266,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t*)&sh.tmem;
     griddep_wait();
+    griddep_launch();   // (the next kernel's set-up, where it fits beside this one)
     const int unit = blockIdx.x / CG, units = gridDim.x / CG;
     Walk<MODE, CG> walk(p);
     Tile t;
@@ -227,6 +279,8 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
         unsigned acc_phase = 0;
         for (int id = unit; walk.find(id, t); id += units) {
             const bool empty = MODE == kWeightsGrad && t.rows == 0;
+            Extras<MODE == kLinear, kHalves, kGroups> extras;   // under way while the products are
+            extras.begin(p, t, rank, group, lane);
             if constexpr (kRowsFirst) {
                 // Rows with scales, in a pair: the rows are the lanes of tensor memory, so that a row's scale is one register of the thread
                 // that adds up its sums -- as columns every sum would need another scale, and those loads alone took as long as the
@@ -390,21 +444,14 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                 constexpr int kWidth = gated(MODE) && CG == 2 ? 64 : 128, kPitch = kWidth == 64 ? kNarrow : kWide;
                 constexpr int kVecs = kWidth / 8, kPasses = kRows * kVecs / 128;
                 const int me = threadIdx.x - kFirstResult * 32 - group * 128;   // thread of the column group
-                for (int h = 0; h < (gated(MODE) ? 1 : kHalves); ++h) {
+                const int halves = gated(MODE) || p.span == 128 ? 1 : kHalves;
+                for (int h = 0; h < halves; ++h) {
                     const int f0 = t.f0 + (gated(MODE) ? rank * kWidth : (h + rank) * 128);
                     if (f0 >= p.F) break;
                     const int col = gated(MODE) && CG == 2 ? quarter * 16 + (lane >> 4) * 8 + (lane & 7) : quarter * 32 + lane;
                     // whole rows' pieces, 16 bytes per thread: rows and features of this thread's vectors
                     const int vec_f = f0 + me % kVecs * 8, vec_row = me / kVecs;
                     const bool vec_in = vec_f < p.F;
-                    uint4 ahead[kPasses];
-                    auto fetch = [&](int c) {   // the residual's next rows
-#pragma unroll
-                        for (int i = 0; i < kPasses; ++i) {
-                            const int r = c + vec_row + i * (128 / kVecs);
-                            ahead[i] = vec_in && r < t.rows ? ld_vec(p.residual + (int64_t)(t.row + r) * p.F + vec_f) : make_uint4(0, 0, 0, 0);
-                        }
-                    };
                     auto put_out = [&](uint16_t* to, int64_t pitch, const uint8_t* from, int c) {
 #pragma unroll
                         for (int i = 0; i < kPasses; ++i) {
@@ -413,14 +460,9 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                                 st_vec(to + (t.row + c + r) * pitch + vec_f, *reinterpret_cast<const uint4*>(from + r * kPitch + me % kVecs * 16));
                         }
                     };
-                    float bias = 0.0f;
-                    if constexpr (MODE == kLinear) {
-                        if (p.bias && f0 + col < p.F)
-                            bias = __uint_as_float((uint32_t)ld_plain(p.bias + (int64_t)t.e * p.F + f0 + col) << 16);
-                        if (p.residual) fetch(group * kRows);
-                    }
+                    const float bias = MODE != kLinear ? 0.0f : h == 0 ? extras.bias[0] : extras.bias[1];
                     for (int c = group * kRows; c < t.rows; c += kGroups * kRows) {
-                        const bool last = c + kGroups * kRows >= t.rows && (gated(MODE) || h == kHalves - 1 || f0 + 128 >= p.F);
+                        const bool last = c + kGroups * kRows >= t.rows && (h == halves - 1 || f0 + 128 >= p.F);
                         uint8_t* tile = tiles + flip * kTile;
                         float v[16];
                         if constexpr (gated(MODE) && CG == 1) tmem_ld8x2(d + c, d + p.most + c, v, v + 8);
@@ -463,21 +505,20 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                                 }
                                 act_values<16>(v, p.act);
                                 if (p.row_scale) {
-                                    const float scale = lane < 16 && c + lane < t.rows ? ld_plain(p.row_scale + t.row + c + lane) : 0.0f;
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) v[i] *= __shfl_sync(0xffffffffu, scale, i);
+                                    for (int i = 0; i < 16; ++i) v[i] *= __shfl_sync(0xffffffffu, extras.scale, i);
                                 }
                                 if (p.residual) {
                                     // through the tile, where every thread finds the values of its own feature
 #pragma unroll
                                     for (int i = 0; i < kPasses; ++i)
-                                        *reinterpret_cast<uint4*>(tile + (vec_row + i * (128 / kVecs)) * kPitch + me % kVecs * 16) = ahead[i];
-                                    if (c + kGroups * kRows < t.rows) fetch(c + kGroups * kRows);
+                                        *reinterpret_cast<uint4*>(tile + (vec_row + i * (128 / kVecs)) * kPitch + me % kVecs * 16) = extras.rows[i];
                                     group_sync(1 + group, 128);
 #pragma unroll
                                     for (int i = 0; i < 16; ++i)
                                         v[i] += __uint_as_float((uint32_t) * reinterpret_cast<const uint16_t*>(at + i * kPitch) << 16);
                                 }
+                                extras.next(p, t, rank);
                             }
 #pragma unroll
                             for (int i = 0; i < 16; ++i) put_bf16(at + i * kPitch, v[i]);
@@ -507,6 +548,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
     // step took 60 cycles longer, of 512.
     const bool lead = elect_one();
     const uint32_t ring0 = smem_u32(ring);
+    const uint32_t a_bytes = kHalves == 2 && !gated(MODE) && p.span == 128 ? kHalfBytes : kHalves * kHalfBytes;
     if (warp == 0) {
         // ------------------------------------------------------------------ loads
         int s = 0, used = 0, ends = 0;
@@ -521,7 +563,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
         };
         for (int id = unit; ok && walk.find(id, t); id += units) {
             const int K = MODE == kWeightsGrad ? t.rows : p.K;
-            const bool two = kHalves == 2 && (gated(MODE) || t.f0 + 128 < p.F);
+            const bool two = kHalves == 2 && (gated(MODE) || (p.span == 256 && t.f0 + 128 < p.F));
             const int f0 = t.f0 + rank * (gated(MODE) ? 64 : 128), fb0 = t.fb0 + rank * 128;
             // (in a pair each CTA brings one half of the rows, or of x's features)
             const int mine = CG == 1 ? t.rows : (t.rows + 31) / 32 * 16, row0 = t.row + rank * mine;
@@ -533,7 +575,7 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                     for (int k0 = 0; k0 < K; k0 += kStepK) {
                         ok = thread_wait<CG>(&sh.empty[s], phase ^ 1, &sh, p.status);
                         if (!ok) break;
-                        const uint32_t a = ring0 + s * p.stage_bytes, b = a + kHalves * kHalfBytes;
+                        const uint32_t a = ring0 + s * p.stage_bytes, b = a + a_bytes;
                         uint32_t bar = CG == 1 ? smem_u32(&sh.full[s]) : first_of_pair(&sh.full[s]);
                         if (kMends && K - k0 < kStepK) {   // each CTA counts its own last rows, which have to be mended
                             uint64_t* end = &sh.ends[ends++ % kMaxRing];
@@ -596,11 +638,11 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
         bool ok = true;
         // (the first stage's operands; the address is the low end of a descriptor, and all of shared memory fits there)
         const uint64_t a0 = kAcross ? operand(ring0, 8192, 1024) : operand(ring0, 16, 1024);
-        const uint64_t b0 = MODE == kWeightsGrad ? operand(ring0 + kHalves * kHalfBytes, 8192, 1024) : operand(ring0 + kHalves * kHalfBytes, 16, 1024);
+        const uint64_t b0 = MODE == kWeightsGrad ? operand(ring0 + a_bytes, 8192, 1024) : operand(ring0 + a_bytes, 16, 1024);
         constexpr int kPartA = (kAcross ? 2048 : 32) >> 4, kPartB = (MODE == kWeightsGrad ? 2048 : 32) >> 4;   // 16 of the contraction
         for (int id = unit; rank == 0 && ok && walk.find(id, t); id += units) {
             const int K = MODE == kWeightsGrad ? t.rows : p.K;
-            const bool two = kHalves == 2 && (gated(MODE) || t.f0 + 128 < p.F);
+            const bool two = kHalves == 2 && (gated(MODE) || (p.span == 256 && t.f0 + 128 < p.F));
             const int n = MODE == kWeightsGrad || kRowsFirst ? 256 : (t.rows + 16 * CG - 1) / (16 * CG) * (16 * CG);
             const uint32_t idesc = instruction(128 * CG, n, kAcross, MODE == kWeightsGrad);
             if (lead && K > 0) {
@@ -689,7 +731,6 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
     if constexpr (CG == 1) __syncthreads();
     else pair_sync();
     tc_fence_after();
-    griddep_launch();
     if (warp == 1) tmem_free<CG>(tmem, kColumns);
 }
 
@@ -940,7 +981,10 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     cudaError_t e = device_facts(&dev);
     if (e != cudaSuccess) return e;
     constexpr int kHalves = CG == 1 ? 2 : 1;
-    p.stage_bytes = kHalves * kHalfBytes + p.most / CG * 128;
+    p.span = gated(MODE) ? 128 : 256;
+    // Single CTAs: narrow tiles where wide ones would not go round the SMs four times.
+    if (CG == 1 && (MODE == kLinear || MODE == kRowsGrad) && (int64_t)p.seg.E * ((p.F + 255) / 256) < 4 * dev.sms) p.span = 128;
+    p.stage_bytes = (p.span == 128 && !gated(MODE) ? 1 : kHalves) * kHalfBytes + p.most / CG * 128;
     p.accs = 2 * kHalves * p.most <= kColumns ? 2 : 1;
     // a tile of results per column group, and one for each array of saved products (the gated block in pairs has room for two in turn)
     p.tiles = p.pre ? (gated(MODE) ? 3 : 2) : gated(MODE) ? 2 : 1;
