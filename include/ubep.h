@@ -478,7 +478,7 @@ typedef struct {
  * in expert order.  In sharded use (ubep_set_peers) these are this rank's experts and its
  * region alone: num_ranks = 1, arrays [1, cap, width].  Nothing is launched.
  */
-int ubep_expert_rows(ubep_buffer_t *buf, ubep_expert_rows_t *rows /*[host]*/);
+int ubep_expert_segments(ubep_buffer_t *buf, ubep_expert_rows_t *rows /*[host]*/);
 
 enum { UBEP_ACT_NONE = 0, UBEP_ACT_SILU = 1, UBEP_ACT_GELU = 2 /* x Phi(x) */, UBEP_ACT_RELU = 3 };
 

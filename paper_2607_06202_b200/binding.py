@@ -50,7 +50,7 @@ EXPORTS = ["ubep_buffer_bytes", "ubep_buffer_create", "ubep_buffer_destroy", "ub
            "ubep_sync_wire_bytes", "ubep_sync_attach", "ubep_dispatch_sync", "ubep_sync_view",
            "ubep_sync_scan_sentinel",
            "ubep_set_peers", "ubep_dispatch_sharded", "ubep_wait_arrivals", "ubep_combine_sharded",
-           "ubep_route", "ubep_route_backward", "ubep_expert_rows", "ubep_expert_gated", "ubep_expert_gated_backward",
+           "ubep_route", "ubep_route_backward", "ubep_expert_segments", "ubep_expert_gated", "ubep_expert_gated_backward",
            "ubep_expert_linear", "ubep_expert_linear_backward"]
 UBEP_LOGITS_F32, UBEP_LOGITS_BF16 = 0, 1
 UBEP_ACT_NONE, UBEP_ACT_SILU, UBEP_ACT_GELU, UBEP_ACT_RELU = 0, 1, 2, 3
@@ -133,7 +133,7 @@ def load() -> ctypes.CDLL:
     lib.ubep_route_backward.restype = ctypes.c_int
     lib.ubep_route_backward.argtypes = [vp, ctypes.c_int, vp, vp, i32, i32, i32, i32, vp, i32, vp]
     rowsp = ctypes.POINTER(ubep_expert_rows_t)
-    lib.ubep_expert_rows.restype, lib.ubep_expert_rows.argtypes = ctypes.c_int, [vp, rowsp]
+    lib.ubep_expert_segments.restype, lib.ubep_expert_segments.argtypes = ctypes.c_int, [vp, rowsp]
     lib.ubep_expert_gated.restype = ctypes.c_int
     lib.ubep_expert_gated.argtypes = [rowsp, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp, vp]
     lib.ubep_expert_gated_backward.restype = ctypes.c_int
@@ -401,9 +401,9 @@ def ubep_combine_sharded(buf, y_peers: torch.Tensor, topk_w: torch.Tensor, T: in
            "ubep_combine_sharded", buf)
 
 
-def ubep_expert_rows(buf) -> ubep_expert_rows_t:
+def ubep_expert_segments(buf) -> ubep_expert_rows_t:
     rows = ubep_expert_rows_t()
-    _check(load().ubep_expert_rows(buf, ctypes.byref(rows)), "ubep_expert_rows", buf)
+    _check(load().ubep_expert_segments(buf, ctypes.byref(rows)), "ubep_expert_segments", buf)
     return rows
 
 
@@ -562,10 +562,10 @@ class Buffer:
             _check(rc, "ubep_combine", self.handle)
         return out
 
-    def expert_rows(self) -> ExpertRows:
+    def expert_segments(self) -> ExpertRows:
         """The segments the last dispatch left, for the experts' calls (one row per (token, slot): not with dedup).  After
         ``ubep_set_peers`` they are those of this rank alone, on arrays [1, cap, width]."""
-        r = ubep_expert_rows(self.handle)
+        r = ubep_expert_segments(self.handle)
         base = self.arena.data_ptr()
 
         def words(ptr, n):

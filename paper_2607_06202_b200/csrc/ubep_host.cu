@@ -917,7 +917,7 @@ int ubep_route_backward(const void* logits, int logits_type, const int32_t* topk
     });
 }
 
-int ubep_expert_rows(ubep_buffer_t* buf, ubep_expert_rows_t* rows) {
+int ubep_expert_segments(ubep_buffer_t* buf, ubep_expert_rows_t* rows) {
     if (!buf || !rows || buf->cfg.dedup) return UBEP_ERR_ARG;
     const ubep_config_t& c = buf->cfg;
     const bool one = buf->my_rank >= 0;   // sharded use: this rank's experts

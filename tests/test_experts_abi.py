@@ -84,7 +84,7 @@ def test_route_arguments(lib):
 
 
 def test_rows_of_no_buffer(lib):
-    assert lib.ubep_expert_rows(None, _rows()) == B.UBEP_ERR_ARG
+    assert lib.ubep_expert_segments(None, _rows()) == B.UBEP_ERR_ARG
 
 
 def test_tensors_on_the_host_are_refused(lib):
