@@ -414,21 +414,20 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                     const int f = t.f0 + (h + rank) * 128 + quarter * 32;
                     for (int c = group * 128; c < group * 128 + 128; c += 64) {
                         if (f >= p.F || t.fb0 + c >= p.FB) break;
-                        if (lane == 0) bulk_wait_read<0>();
+                        float v[64];
+                        if (empty) {
+#pragma unroll
+                            for (int j = 0; j < 64; ++j) v[j] = 0.0f;
+                        } else {
+                            tmem_ld64(d + h * p.most + c, v);
+                        }
+                        give_back(c == group * 128 + 64 && (h == kHalves - 1 || f + 128 >= p.F));
+                        if (lane == 0) bulk_wait_read<0>();   // (the tile's last copy has read it)
                         __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float v[16];
-                            if (empty) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = 0.0f;
-                            } else {
-                                tmem_ld16(d + h * p.most + c + i * 16, v);
-                            }
+                        for (int i = 0; i < 8; ++i)
                             // (16-byte pieces in the order of the 128-byte swizzle: conflict-free)
-                            *reinterpret_cast<uint4*>(tiles + lane * 128 + (((2 * i) ^ (lane & 7)) << 4)) = pack8(v);
-                            *reinterpret_cast<uint4*>(tiles + lane * 128 + (((2 * i + 1) ^ (lane & 7)) << 4)) = pack8(v + 8);
-                        }
+                            *reinterpret_cast<uint4*>(tiles + lane * 128 + ((i ^ (lane & 7)) << 4)) = pack8(v + i * 8);
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {

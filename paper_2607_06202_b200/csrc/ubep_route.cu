@@ -1,10 +1,11 @@
 // Router: the k largest logits of every token and their softmax weights, and the gradient with respect to the logits.
 //
 // One warp per token.  Forward: every lane makes a number of each of its logits whose order is (value, then lower expert id), 0 for a
-// masked one, and sorts its own few in registers; a round takes the largest of the lanes' first ones with a warp reduction, and
-// the lane that held it moves up.  Of bf16 logits value and id fit in 32 bits, one reduction; fp32 logits take 64 and two.  A
-// round costs a dozen instructions; searched anew in every round, 16384 tokens x 256 experts with k = 8 took 18.0 us.  A logit is
-// read once, the table and weights are written once.
+// masked one, and knows its two largest; a round takes the largest of the warp with a reduction, and the lane that held it moves
+// its second one up, or looks its numbers over again where that one is gone too.  Of bf16 logits value and id fit in 32 bits, one
+// reduction; fp32 logits take 64 and two.  A logit is read once, the table and weights are written once, and integer
+// instructions are what bounds it.  16384 tokens x 256 experts of bf16, k = 8: searched anew in every round 18.0 us, every lane's
+// numbers sorted 10.8, the lanes' sorted lists merged over the warp 13.1.
 #include <cstdint>
 
 #include "ubep_common.cuh"
@@ -26,11 +27,11 @@ __device__ __forceinline__ void put(uint16_t* p, float v) {
     *p = *reinterpret_cast<const uint16_t*>(&b);
 }
 
-// Integers in the order of the values; 0 for minus infinity and for no number.  (Both zeros are the same value.)
+// Integers in the order of the values; 0 for minus infinity and for no number.  (Both zeros are the same value: the sum with zero.)
 __device__ __forceinline__ unsigned order_key(float v) {
-    if (!(v > -INFINITY)) return 0u;
-    const unsigned u = v == 0.0f ? 0u : __float_as_uint(v);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const unsigned u = __float_as_uint(__fadd_rn(v, 0.0f));
+    const unsigned key = u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+    return v > -INFINITY ? key : 0u;
 }
 __device__ __forceinline__ float key_value(unsigned key) {
     if (key == 0u) return -INFINITY;
@@ -89,24 +90,22 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const T* logits, i
             const int e = i * 32 + lane;
             mine[i] = e < E ? R::make(as_float(ld_plain(row + e)), e) : 0;
         }
-        // sorted, largest first
+    }
+    Num best = 0, second = 0;   // of this lane; second = 0: none, or not known
+    if constexpr (V > 0) {
 #pragma unroll
-        for (int i = 1; i < V; ++i)
-#pragma unroll
-            for (int j = i; j > 0; --j) {
-                const Num a = mine[j - 1], b = mine[j];
-                mine[j - 1] = a > b ? a : b;
-                mine[j] = a > b ? b : a;
-            }
+        for (int i = 0; i < V; ++i) {
+            const Num low = mine[i] < best ? mine[i] : best;
+            best = mine[i] < best ? best : mine[i];
+            second = low < second ? second : low;
+        }
     }
     Num chosen = 0, last = ~(Num)0, top = 0;
     float total = 0.0f;
     for (int j = 0; j < k; ++j) {
-        Num best = 0;
-        if constexpr (V > 0) {
-            best = mine[0];
-        } else {
+        if constexpr (V == 0) {
             // the largest behind the last one taken
+            best = 0;
             for (int e = lane; e < E; e += 32) {
                 const Num n = R::make(as_float(ld_plain(row + e)), e);
                 if (n > best && n < last) best = n;
@@ -129,9 +128,15 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const T* logits, i
         if (lane == j) chosen = last;
         if constexpr (V > 0) {
             if (best == last) {
+                best = second;
+                second = 0;
+                if (best == 0) {
 #pragma unroll
-                for (int i = 0; i + 1 < V; ++i) mine[i] = mine[i + 1];
-                mine[V - 1] = 0;
+                    for (int i = 0; i < V; ++i) {
+                        const Num n = mine[i] < last ? mine[i] : 0;
+                        best = n > best ? n : best;
+                    }
+                }
             }
         }
     }
