@@ -5,12 +5,16 @@
 //   rows' gradient   D^T[feature, row] = sum_n W[n, feature] dz[row, n]  W across it
 //   weights' gradient   D[n, feature] = sum_row dz[row, n] x[row, feature]   both across it, the rows being the contraction
 //
-// One persistent kernel, one CTA per SM: a warp loads operand tiles with tensor-map copies into a ring in shared memory, a warp
-// issues tcgen05.mma, eight warps turn sums in tensor memory into results.  The rows are the N dimension of the
-// instruction (a multiple of 16), the features its M (128 per CTA): a segment of 139 rows costs 144, where rows as M would
-// cost 256, and sixteen rows of a decode step cost sixteen.  Each tile of rows is multiplied with two tiles of features (gate and
-// up of the same features, or 256 features of one matrix), which halves the shared-memory and L2 traffic per
-// multiplication: a step of 64 of the contraction brings 64 KB for 1024 cycles of the tensor cores.
+// One persistent kernel, one CTA per SM: a thread loads operand tiles with tensor-map copies into a ring in shared memory, a thread
+// issues tcgen05.mma, eight or sixteen warps turn sums in tensor memory into results.  The rows are the N dimension of the
+// instruction, the features its M: a segment of 139 rows costs 144 (160 in pairs), where rows as M would cost 256, and sixteen rows of a
+// decode step cost sixteen.
+//   single CTAs (few rows per expert): two tiles of 128 features, one of up to 64 rows; 32 KB of weights per step of 64 of the
+//     contraction.  Reading the weights bounds them: 32 experts of 7168 x 2048, 16 rows each, 270 - 282 us for 1.88 GB.
+//   pairs (cta_group::2): 256 features x up to 256 rows, half of either brought by each CTA, two accumulators, so that the results
+//     of one tile leave while the next is multiplied.  A step brings 32 KB per CTA for 512 cycles of the tensor cores, about what an SM
+//     takes in from L2.  8 experts of 4096 x 2048, 1024 rows each: gated 176 - 189 us (1460 - 1560 TFLOP/s), tensor cores active 93 % of
+//     the time, linear 96 - 99, the rows' gradient 99 - 104, the weights' 99 - 104; one cuBLAS product of the same rows 93 - 95.
 #include <cstdint>
 #include <atomic>
 
@@ -1001,7 +1005,10 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
 
 // The segments of a call are not known to the host, their capacity is.
 int64_t rows_each(const ubep_expert_rows_t& r) { return (int64_t)r.num_ranks * r.rows_per_rank_cap / r.num_experts; }
-// Pairs of CTAs where there are rows enough to multiply; single CTAs where the weights are most of the traffic.
+// Pairs of CTAs where there are rows enough to multiply; single CTAs, with more of the weights under way, where reading those is all
+// there is to do.  Single against pairs, 32 experts of 4096 x 2048, rows each: gated 64: 172 and 176 us, 96: 195 and 182, 128: 202 and
+// 186; linear 64: 90 and 92, 96: 144 and 96; FP8 rows 32: 181 and 231, 64: 191 and 238, 128: 266 and 261; weights' gradient 32: 104 and 112,
+// 64: 98 and 110, 96: 124 and 132, 128: 142 and 113; the rows' gradient 32: 88.7 and 85.9, 96: 132 and 95.
 bool in_pairs(const ubep_expert_rows_t& r) { return rows_each(r) > 64; }
 // Rows per tile.  Small pieces leave room for more stages and a second accumulator.
 int rows_per_tile(const ubep_expert_rows_t& r) { return in_pairs(r) ? 256 : 64; }

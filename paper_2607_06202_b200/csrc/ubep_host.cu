@@ -900,8 +900,10 @@ int ubep_route(const void* logits, int logits_type, int32_t T, int32_t E, int32_
     if (!route_args(logits, logits_type, topk_idx, topk_w, T, E, k)) return UBEP_ERR_ARG;
     if (T == 0) return UBEP_OK;
     return on_device(device, [&](int* n) {
-        *n = 1;
-        return ubep::launch_route(logits, logits_type, T, E, k, renormalize != 0, topk_idx, topk_w, static_cast<cudaStream_t>(cuda_stream));
+        const cudaError_t e = ubep::launch_route(logits, logits_type, T, E, k, renormalize != 0, topk_idx, topk_w,
+                                                 static_cast<cudaStream_t>(cuda_stream));
+        *n = e == cudaSuccess;
+        return e;
     });
 }
 
@@ -911,9 +913,10 @@ int ubep_route_backward(const void* logits, int logits_type, const int32_t* topk
     if (T == 0) return UBEP_OK;
     if (!grad_logits || !aligned16(grad_logits) || grad_logits == logits) return UBEP_ERR_ARG;
     return on_device(device, [&](int* n) {
-        *n = 1;
-        return ubep::launch_route_backward(logits, logits_type, topk_idx, grad_w, T, E, k, renormalize != 0, grad_logits,
-                                           static_cast<cudaStream_t>(cuda_stream));
+        const cudaError_t e = ubep::launch_route_backward(logits, logits_type, topk_idx, grad_w, T, E, k, renormalize != 0,
+                                                          grad_logits, static_cast<cudaStream_t>(cuda_stream));
+        *n = e == cudaSuccess;
+        return e;
     });
 }
 
