@@ -38,8 +38,8 @@ __host__ __device__ constexpr bool gated(int mode) { return mode == kGated || mo
 // A warpgroup with a loading warp, a multiplying warp and (weights' gradient in pairs) one that mends the last rows; the others turn
 // sums into results: in groups of four warps, which share the tile's columns.
 constexpr int kFirstResult = 4;
-__host__ __device__ constexpr int result_groups(int mode) { return mode == kLinear ? 4 : 2; }
-__host__ __device__ constexpr int gemm_threads(int mode) { return 32 * (kFirstResult + 4 * result_groups(mode)); }
+__host__ __device__ constexpr int result_groups(int mode, int cg) { return mode == kLinear || (mode == kGatedScaled && cg == 2) ? 4 : 2; }
+__host__ __device__ constexpr int gemm_threads(int mode, int cg) { return 32 * (kFirstResult + 4 * result_groups(mode, cg)); }
 constexpr int kStepK = 64;               // of the contraction per stage: 128 bytes of bf16, the swizzle's width
 constexpr int kHalfBytes = 128 * 128;    // 128 features of one stage
 constexpr int kMaxRing = 8;
@@ -219,7 +219,7 @@ __device__ __forceinline__ uint4 ld_vec(const uint16_t* p) { return *reinterpret
 __device__ __forceinline__ void st_vec(uint16_t* p, uint4 v) { *reinterpret_cast<uint4*>(p) = v; }
 
 template <int MODE, int CG>
-__global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
+__global__ void __launch_bounds__(gemm_threads(MODE, CG), 1) expert_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                           const __grid_constant__ CUtensorMap map_b,
                                                                           const __grid_constant__ CUtensorMap map_c, const Product p) {
     extern __shared__ uint8_t dynamic[];
@@ -228,11 +228,11 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
     constexpr bool kAcross = MODE == kRowsGrad || MODE == kWeightsGrad;   // the features' operand
     constexpr bool kMends = MODE == kWeightsGrad;
     constexpr bool kScaled = MODE == kGatedScaled;
-    constexpr int kGroups = result_groups(MODE), kTile = tile_bytes(MODE, CG);
+    constexpr int kGroups = result_groups(MODE, CG), kTile = tile_bytes(MODE, CG);
     // Rows with scales, in pairs: a tile's sums are kept in the result warps' registers, which get some of the others'.
-    constexpr bool kRowsFirst = kScaled && CG == 2, kSplits = kRowsFirst || kGroups == 4;
-    // 384 threads x 168 = 128 x 40 + 256 x 232; 640 threads x 96 = 61440, 128 x 48 + 512 x 104 = 59392
-    constexpr int kFewRegisters = kGroups == 2 ? 40 : 48, kManyRegisters = kGroups == 2 ? 232 : 104;
+    constexpr bool kRowsFirst = kScaled && CG == 2, kSplits = kGroups == 4;
+    // 640 threads x 96 = 61440: 128 x 48 + 512 x 104 = 59392, 128 x 32 + 512 x 112 = 61440
+    constexpr int kFewRegisters = kRowsFirst ? 32 : 48, kManyRegisters = kRowsFirst ? 112 : 104;
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~(uintptr_t)1023);
     uint8_t* results = ring + (size_t)p.stages * p.stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -293,9 +293,9 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                 const bool mine = quarter * 32 + lane < half && r < t.rows;
                 const int64_t row = t.row + r;
                 const float* from = p.x_scale + row * groups;
-                float sum[128];
+                float sum[64];
 #pragma unroll
-                for (int i = 0; i < 128; ++i) sum[i] = 0.0f;
+                for (int i = 0; i < 64; ++i) sum[i] = 0.0f;
                 float next = mine ? ld_plain(from) : 0.0f;
                 bool ok = true;
                 for (int g = 0; g < groups; ++g) {
@@ -304,18 +304,18 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                     ok = warp_wait<CG>(&sh.acc_full[acc], acc_phase, &sh, p.status);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * 256 + group * 128;
+                    const uint32_t d = tmem + ((uint32_t)(quarter * 32) << 16) + acc * 256 + group * 64;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float v[64];
-                        tmem_ld64(d + h * 64, v);
+                        float v[32];
+                        tmem_ld32(d + h * 32, v);
                         if (h == 1) {   // all of them have been read: the products may go on
                             tc_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive_pair_relaxed(first_of_pair(&sh.acc_empty[acc]));
                         }
 #pragma unroll
-                        for (int i = 0; i < 64; i += 2) fma_two(sum + h * 64 + i, v + i, scale);
+                        for (int i = 0; i < 32; i += 2) fma_two(sum + h * 32 + i, v + i, scale);
                     }
                     if (++acc == p.accs) {
                         acc = 0;
@@ -324,8 +324,8 @@ __global__ void __launch_bounds__(gemm_threads(MODE), 1) expert_kernel(const __g
                 }
                 if (group_or(1 + group, 128, !ok)) break;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int f = t.f0 + group * 64 + i * 8;
+                for (int i = 0; i < 4; ++i) {
+                    const int f = t.f0 + group * 32 + i * 8;
                     if (f >= p.F || !mine) continue;
                     float *g = sum + i * 16, *u = g + 8;
                     if (p.pre) {
@@ -991,7 +991,7 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     p.accs = 2 * kHalves * p.most <= kColumns ? 2 : 1;
     // a tile of results per column group, and one for each array of saved products (the gated block in pairs has room for two in turn)
     p.tiles = p.pre ? (gated(MODE) ? 3 : 2) : gated(MODE) ? 2 : 1;
-    const int tiles = result_groups(MODE) * (MODE == kWeightsGrad ? 1 : p.tiles) * tile_bytes(MODE, CG);
+    const int tiles = result_groups(MODE, CG) * (MODE == kWeightsGrad ? 1 : p.tiles) * tile_bytes(MODE, CG);
     const int room = dev.smem - 1024 - (int)sizeof(Shared) - tiles;
     p.stages = room / p.stage_bytes;
     if (p.stages > kMaxRing) p.stages = kMaxRing;
@@ -1000,7 +1000,7 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     static std::atomic<int> granted[kAttrDevices];
     e = allow_dynamic_smem(reinterpret_cast<const void*>(expert_kernel<MODE, CG>), smem, granted);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE), (size_t)smem, st, false, CG, a, b, c, p);
+    return launch_overlapped(expert_kernel<MODE, CG>, dev.sms / CG * CG, gemm_threads(MODE, CG), (size_t)smem, st, false, CG, a, b, c, p);
 }
 
 // The segments of a call are not known to the host, their capacity is.
