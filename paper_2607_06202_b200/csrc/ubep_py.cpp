@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -106,6 +107,20 @@ bool stream_arg(PyObject* o, void** st) {
     *st = PyLong_AsVoidPtr(h);
     Py_DECREF(h);
     return !PyErr_Occurred();
+}
+
+// Memory for work on stream `st`, `current` being torch's.  It comes from the pool of `st` itself: the allocator hands a block out again
+// as soon as it is given back, and only the stream it was given back on is sure to be done with it by then -- from the current
+// stream's pool a kernel on another one would write what the current stream may still work on.  `kept`: the caller gets it, who
+// may use it on the current stream as well, so what that has under way is waited for before the block goes to anybody else.
+at::Tensor memory_on(void* st, const c10::cuda::CUDAStream& current, c10::IntArrayRef shape, at::ScalarType type, bool kept) {
+    const c10::Device dev = current.device();
+    if (st == static_cast<void*>(current.stream())) return at::detail::empty_cuda(shape, type, dev, c10::nullopt);
+    if (st == reinterpret_cast<void*>(1)) st = nullptr;   // cudaStreamLegacy: the default stream by its other name
+    const c10::cuda::CUDAStreamGuard on(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), dev.index()));
+    at::Tensor t = at::detail::empty_cuda(shape, type, dev, c10::nullopt);
+    if (kept) t.record_stream(current.unwrap());
+    return t;
 }
 
 bool want_args(Py_ssize_t n, Py_ssize_t want) {
@@ -294,28 +309,18 @@ PyObject* refused_or_raised() {
     return nullptr;
 }
 
-// Where the tensors of a call live and which stream it runs on; temporaries are tied to that stream.
+// Where the tensors of a call live and which stream it runs on.
 struct Place {
-    c10::Device dev{c10::kCUDA, 0};
+    c10::Device dev;
+    c10::cuda::CUDAStream current;   // torch's, of that device
     void* stream = nullptr;
-    bool foreign = false;   // not torch's current stream
-    explicit Place(const at::Tensor& any, PyObject* s) : dev(any.device()) {
-        const auto current = c10::cuda::getCurrentCUDAStream(dev.index());
-        if (s == Py_None) {
-            stream = current.stream();
-            return;
-        }
-        if (!stream_arg(s, &stream)) throw Raised();
-        foreign = stream != static_cast<void*>(current.stream());
+    Place(const at::Tensor& any, PyObject* s) : dev(any.device()), current(c10::cuda::getCurrentCUDAStream(dev.index())) {
+        if (s == Py_None) stream = current.stream();
+        else if (!stream_arg(s, &stream)) throw Raised();
     }
-    at::Tensor make(c10::IntArrayRef shape, at::ScalarType type) const { return at::detail::empty_cuda(shape, type, dev, c10::nullopt); }
-    // memory of this call alone: given back when it returns, so the allocator has to know who still works on it
-    at::Tensor scratch(c10::IntArrayRef shape, at::ScalarType type) const {
-        at::Tensor t = make(shape, type);
-        if (foreign)
-            t.record_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), dev.index()).unwrap());
-        return t;
-    }
+    at::Tensor make(c10::IntArrayRef shape, at::ScalarType type) const { return memory_on(stream, current, shape, type, true); }
+    // memory of this call alone, given back when it returns
+    at::Tensor scratch(c10::IntArrayRef shape, at::ScalarType type) const { return memory_on(stream, current, shape, type, false); }
 };
 
 const at::Tensor& need(PyObject* o, const char* name) {
