@@ -216,8 +216,8 @@ PyObject* py_combine_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!handle_arg(a[0], &buf) || !tensor_arg(a[1], &y) || !tensor_arg(a[2], &w) || !rows_of(a[2], &T) ||
             !int_arg(a[3], &hidden) || !int_arg(a[4], &device) || !stream_arg(a[5], &st))
             return nullptr;
-        at::Tensor out = at::detail::empty_cuda({(int64_t)T, (int64_t)hidden}, at::kBFloat16,
-                                                c10::Device(c10::kCUDA, (c10::DeviceIndex)device), c10::nullopt);
+        const auto current = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device);
+        at::Tensor out = memory_on(st, current, {(int64_t)T, (int64_t)hidden}, at::kBFloat16, true);
         void* po = out.data_ptr();
         const int rc = without_gil([&] { return f_combine(buf, y, static_cast<const float*>(w), T, po, st); });
         if (rc != UBEP_OK) return PyLong_FromLong(rc);
@@ -259,10 +259,9 @@ PyObject* py_layout_new(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!handle_arg(a[0], &buf) || !tensor_arg(a[1], &idx) || !rows_of(a[1], &T) || !int_arg(a[2], &R) ||
             !int_arg(a[3], &E) || !int_arg(a[4], &device) || !stream_arg(a[5], &st))
             return nullptr;
-        const c10::Device dev(c10::kCUDA, (c10::DeviceIndex)device);
-        at::Tensor parts[3] = {at::detail::empty_cuda({(int64_t)R}, at::kInt, dev, c10::nullopt),
-                               at::detail::empty_cuda({(int64_t)E}, at::kInt, dev, c10::nullopt),
-                               at::detail::empty_cuda({(int64_t)T, (int64_t)R}, at::kByte, dev, c10::nullopt)};
+        const auto current = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device);
+        at::Tensor parts[3] = {memory_on(st, current, {(int64_t)R}, at::kInt, true), memory_on(st, current, {(int64_t)E}, at::kInt, true),
+                               memory_on(st, current, {(int64_t)T, (int64_t)R}, at::kByte, true)};
         void* po[3] = {parts[0].data_ptr(), parts[1].data_ptr(), parts[2].data_ptr()};
         const int rc = without_gil([&] {
             return f_layout(buf, static_cast<const int32_t*>(idx), T, static_cast<int32_t*>(po[0]),

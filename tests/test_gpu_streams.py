@@ -113,3 +113,28 @@ def test_captured_with_a_stream_by_argument():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got[R.mine], want[R.mine])
+
+
+def test_combine_and_layout_allocate_on_the_call_s_stream():
+    T, H, E, R, k = 2048, 2048, 64, 8, 4
+    gen = _gen(8)
+    x = torch.randn((T, H), generator=gen, device="cuda").to(torch.bfloat16)
+    idx, w = B.route(torch.randn((T, E), generator=gen, device="cuda"), k)
+    buf = B.Buffer(num_ranks=R, num_experts=E, hidden=H, topk=k, max_tokens=T, rows_per_rank_cap=T * k)
+    buf.dispatch(x, idx, w)
+    y = buf.recv_x.view(torch.bfloat16)
+    layout, out = buf.get_dispatch_layout(idx), buf.combine(y, w)
+    side = a_side_stream()
+    done = behind_a_queue(out.shape, torch.bfloat16, float("nan"))
+    got = buf.combine(y, w, stream=side)
+    side.synchronize()
+    assert not done.query()                  # the fill comes after the call's kernels
+    torch.cuda.synchronize()
+    assert torch.equal(got, out)
+    side = a_side_stream()
+    behind_a_queue((T, R), torch.uint8, 9)
+    parts = buf.get_dispatch_layout(idx, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for a, b in zip(parts, layout):
+        assert torch.equal(a, b)
