@@ -8,8 +8,8 @@ namespace ubep {
 enum { kActNone = 0, kActSilu = 1, kActGelu = 2, kActRelu = 3 };
 
 // Sums and activations are taken in 32 bits.  The exponential and the quotient are the fast ones, off by (2 + 1.2 |argument|) and 2 units of
-// 2^-23; with them gelu is good to (12 + 0.9 z^2) units of its value, 2e-5 at z = -13 -- far inside the half step (2^-8 at most) of the bf16
-// results, in the tail too.
+// 2^-23; with them silu is good to (8 + 1.2 |z|) units of its value (below z = -87, where the quotient is under 2^-126, it is 0) and gelu to
+// (12 + 0.9 z^2), 2e-5 at z = -13 -- far inside the half step (2^-8 at most) of the bf16 results, in the tails too.
 // The normal distribution's Phi(z), and exp(-z^2 / 2): Phi(-|z|) = exp(-z^2 / 2) q(t), t = 1 / (1 + 0.23334524 |z|), with the polynomial q fitted
 // here by linear programming to exp(z^2 / 2) Phi(-|z|) for |z| up to 14, so that the largest error relative to the value is least
 // (7e-8; 4 units of 2^-23 when evaluated in 32 bits).  The tail is a product, nothing cancels in it.  erff made the epilogue of a

@@ -3,7 +3,9 @@ with the identity, so the argument is exact.
 
 Units are 2^-23.  The exponential is off by 2 + 1.173 |argument| (the CUDA programming guide's bound of __expf), the quotient by 2.
 gelu: the polynomial 4, the quotient's 2 twice (the polynomial goes at most with the square of its argument), the rounding of z^2 as 0.5 z^2 / 2,
-products and the rest 2: 12 + 1.7 z^2 / 2.  The slope is a sum of Phi and z phi, each as good."""
+products and the rest 2: 12 + 1.7 z^2 / 2.  The slope is a sum of Phi and z phi, each as good.
+silu: the exponential of -|z|, the quotient and three roundings, 8 + 1.173 |z|.  The slope p (1 + z (1 - p)) takes two such factors: twice that, of
+p (1 + |z| (1 - p))."""
 import pytest
 import torch
 
@@ -20,6 +22,9 @@ def act_exact(z, act):
     if act == "gelu":
         c = 0.5 * torch.special.erfc(-z * 0.5 ** 0.5)
         return z * c, c + z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+    if act == "silu":
+        p, rest = 1 / (1 + torch.exp(-z)), 1 / (1 + torch.exp(z))
+        return z * p, p * (1 + z * rest)
     return (torch.relu(z), (z > 0).double()) if act == "relu" else (z, torch.ones_like(z))
 
 
@@ -38,7 +43,7 @@ def rows_of(x):
 
 
 def units(z, act):
-    return (12 + 0.85 * z * z if act == "gelu" else torch.zeros_like(z)) * UNIT
+    return {"gelu": 12 + 0.85 * z * z, "silu": 8 + 1.173 * z.abs()}.get(act, torch.zeros_like(z)) * UNIT
 
 
 def step(v):
@@ -52,7 +57,7 @@ def check(name, got, want, tol):
     assert not bad.any(), f"{name}: {int(bad.sum())} of {bad.numel()}, worst {float((off / tol).max()):.3g} of the tolerance"
 
 
-@pytest.mark.parametrize("act,most", [("gelu", 13.0), ("relu", 100.0), ("none", 100.0)])
+@pytest.mark.parametrize("act,most", [("gelu", 13.0), ("silu", 100.0), ("relu", 100.0), ("none", 100.0)])
 def test_values_and_slopes(act, most):
     x = arguments(most)
     z, one = x.double(), torch.eye(8, dtype=torch.bfloat16, device="cuda")[None]
@@ -80,6 +85,8 @@ def test_values_and_slopes(act, most):
     size = slope.abs()
     if act == "gelu":
         size = 0.5 * torch.special.erfc(-z * 0.5 ** 0.5) + (z * torch.exp(-z * z / 2)).abs() * 0.3989422804014327
+    if act == "silu":
+        size = 2 * (1 + z.abs() / (1 + torch.exp(z))) / (1 + torch.exp(-z))
     check("slope", gx, slope, rel * size * (1 + 2.0 ** -8) + step(slope) + LOW * (1 + z.abs()))
     gg = B.expert_gated_backward(rows, wide, w, torch.stack((x, torch.ones_like(x)), 2), torch.ones_like(x), act=act, grad_w=False)[0]
     check("gated slope", gg[..., :8], slope, rel * size * (1 + 2.0 ** -8) + step(slope) + LOW * (1 + z.abs()))
