@@ -461,6 +461,8 @@ int ubep_route_backward(const void *logits /*[dev]*/, int logits_type, const int
  * [num_ranks, rows_per_rank_cap, width]; expert e of rank r = e / (num_experts / num_ranks) has rows
  * offset[e] .. offset[e] + count[e] - 1 of region r (what passes the region's end is left out,
  * as in dispatch).  Rows of no segment are neither read nor written; segments may not overlap.
+ * Limits: 65535 experts, num_ranks * rows_per_rank_cap below 2^31, widths multiples of 8 and at most 2^20, and less than 2^40
+ * bytes in one expert's weights (both matrices of the gated block) and in one array of bf16 rows; UBEP_ERR_ARG beyond them.
  */
 typedef struct {
     const int32_t *offset;     /* [dev] [num_experts]                                          */

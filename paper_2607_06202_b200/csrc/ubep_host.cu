@@ -466,12 +466,16 @@ bool arrays(std::initializer_list<const void*> needed, std::initializer_list<con
     return true;
 }
 
-bool expert_args(const ubep_expert_rows_t* r, int32_t in, int32_t out, int act) {
+// `out` features of each of an expert's `matrices`.
+bool expert_args(const ubep_expert_rows_t* r, int32_t in, int32_t out, int matrices, int act) {
     if (!r || !r->offset || !r->count || r->num_experts < 1 || r->num_ranks < 1 || r->num_experts % r->num_ranks != 0) return false;
     if (r->rows_per_rank_cap < 1 || (int64_t)r->num_ranks * r->rows_per_rank_cap > INT32_MAX) return false;
     if (r->num_experts > 65535 || r->device < 0) return false;
-    // (1 << 28 features: a tensor map's strides stay below its limit, and feature numbers in 32 bits)
+    // (features: tile numbers, features x features / 2^15 of them per expert, stay in 32 bits)
     if (in < 8 || out < 8 || in % 8 != 0 || out % 8 != 0 || in > (1 << 20) || out > (1 << 20)) return false;
+    // strides of a tensor map: from one expert's weights to the next one's, and all rows of an array
+    const int64_t most = (int64_t)1 << 40, outs = (int64_t)matrices * out, rows = (int64_t)r->num_ranks * r->rows_per_rank_cap;
+    if (2 * outs * in >= most || 2 * rows * (in > outs ? in : outs) >= most) return false;
     return act >= UBEP_ACT_NONE && act <= UBEP_ACT_RELU;
 }
 
@@ -937,7 +941,7 @@ int ubep_expert_segments(ubep_buffer_t* buf, ubep_expert_rows_t* rows) {
 
 int ubep_expert_gated(const ubep_expert_rows_t* rows, const void* x, const float* x_scale, const void* w, int32_t H, int32_t I, int act,
                       void* h, void* pre, void* scratch, void* cuda_stream) {
-    if (!expert_args(rows, H, I, act) || !arrays({x, w, h}, {x_scale, pre, scratch})) return UBEP_ERR_ARG;
+    if (!expert_args(rows, H, I, 2, act) || !arrays({x, w, h}, {x_scale, pre, scratch})) return UBEP_ERR_ARG;
     if (x_scale && (H % 128 != 0 || !scratch)) return UBEP_ERR_ARG;
     return on_device(rows->device, [&](int* n) {
         return ubep::launch_expert_gated(*rows, x, x_scale, w, H, I, act, h, pre, scratch, static_cast<cudaStream_t>(cuda_stream), n);
@@ -947,7 +951,7 @@ int ubep_expert_gated(const ubep_expert_rows_t* rows, const void* x, const float
 int ubep_expert_gated_backward(const ubep_expert_rows_t* rows, const void* x, const float* x_scale, const void* w, const void* pre,
                                const void* grad_h, int32_t H, int32_t I, int act, void* grad_pre, void* grad_x, void* grad_w,
                                void* scratch, void* cuda_stream) {
-    if (!expert_args(rows, H, I, act) || !arrays({pre, grad_h, grad_pre}, {x, w, x_scale, grad_x, grad_w, scratch})) return UBEP_ERR_ARG;
+    if (!expert_args(rows, H, I, 2, act) || !arrays({pre, grad_h, grad_pre}, {x, w, x_scale, grad_x, grad_w, scratch})) return UBEP_ERR_ARG;
     if ((grad_x && !w) || (grad_w && !x) || (!grad_x && !grad_w)) return UBEP_ERR_ARG;
     if (grad_w && x_scale && (H % 128 != 0 || !scratch)) return UBEP_ERR_ARG;
     return on_device(rows->device, [&](int* n) {
@@ -958,7 +962,7 @@ int ubep_expert_gated_backward(const ubep_expert_rows_t* rows, const void* x, co
 
 int ubep_expert_linear(const ubep_expert_rows_t* rows, const void* x, const void* w, const void* bias, const float* row_scale,
                        const void* residual, int32_t K, int32_t N, int act, void* y, void* pre, void* cuda_stream) {
-    if (!expert_args(rows, K, N, act) || !arrays({x, w, y}, {bias, row_scale, residual, pre})) return UBEP_ERR_ARG;
+    if (!expert_args(rows, K, N, 1, act) || !arrays({x, w, y}, {bias, row_scale, residual, pre})) return UBEP_ERR_ARG;
     return on_device(rows->device, [&](int* n) {
         return ubep::launch_expert_linear(*rows, x, w, bias, row_scale, residual, K, N, act, y, pre, static_cast<cudaStream_t>(cuda_stream), n);
     });
@@ -967,7 +971,7 @@ int ubep_expert_linear(const ubep_expert_rows_t* rows, const void* x, const void
 int ubep_expert_linear_backward(const ubep_expert_rows_t* rows, const void* x, const void* w, const void* pre, const float* row_scale,
                                 const void* grad_y, int32_t K, int32_t N, int act, void* grad_pre, void* grad_x, void* grad_w,
                                 void* grad_bias, float* grad_row_scale, float* scratch, void* cuda_stream) {
-    if (!expert_args(rows, K, N, act) ||
+    if (!expert_args(rows, K, N, 1, act) ||
         !arrays({grad_y}, {x, w, pre, row_scale, grad_pre, grad_x, grad_w, grad_bias, grad_row_scale, scratch}))
         return UBEP_ERR_ARG;
     if ((grad_bias && !scratch) || (grad_row_scale && N > 16384)) return UBEP_ERR_ARG;
