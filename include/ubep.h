@@ -449,7 +449,8 @@ int ubep_route(const void *logits /*[dev]*/, int logits_type, int32_t T, int32_t
 /*
  * Gradient of the weights with respect to the logits, of all E experts: grad_w [dev] fp32
  * [T, k] in, grad_logits [dev] [T, E] of `logits_type` out (it may not be the logits).  topk_idx as
- * ubep_route left it; slots that hold no expert's id, or the id of an earlier slot, count as empty.
+ * ubep_route left it; slots that hold no expert's id, the id of an earlier slot or that of
+ * a masked expert count as empty.
  * One launch.
  */
 int ubep_route_backward(const void *logits /*[dev]*/, int logits_type, const int32_t *topk_idx /*[dev]*/,

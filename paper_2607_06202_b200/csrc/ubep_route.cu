@@ -183,8 +183,8 @@ __global__ void __launch_bounds__(kRouteThreads) route_grad_kernel(const T* logi
     if (idx < 0 || idx >= E) idx = -1 - lane;
     // a second slot with the same expert counts as empty, as in dispatch
     const bool first = __ffs(__match_any_sync(kFull, idx)) - 1 == lane;
-    const bool used = idx >= 0 && first;
-    const float mine = used ? logit(idx) : -INFINITY;
+    const float mine = idx >= 0 && first ? logit(idx) : -INFINITY;
+    const bool used = mine > -INFINITY;   // (a masked expert has no weight: whatever its slot's gradient is, it is not looked at)
     most = fmaxf(most, mine);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(kFull, most, o));
