@@ -985,8 +985,11 @@ cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const CUt
     if (e != cudaSuccess) return e;
     constexpr int kHalves = CG == 1 ? 2 : 1;
     p.span = gated(MODE) ? 128 : 256;
-    // Single CTAs: narrow tiles where wide ones would not go round the SMs four times.
-    if (CG == 1 && (MODE == kLinear || MODE == kRowsGrad) && (int64_t)p.seg.E * ((p.F + 255) / 256) < 4 * dev.sms) p.span = 128;
+    // Single CTAs: narrow tiles where there is an SM for each of them (one tile of rows per expert).  Narrow against wide, 4096 x 2048 and
+    // 2048 x 2048 weights, 16 rows each, linear (the rows' gradient alike): 4 experts (64 narrow tiles) 19.0 and 23.5 us, 8 of 2048 x 2048
+    // (128) 15.1 and 16.3; with more of them than SMs a few get two, as long as a wide one: 10 experts (160) 43.6 and 37.0, 12 of 2048 x 2048
+    // (192) 24.9 and 21.4, 16 (256) 26.7 and 25.8, 32 (512) 48.6 and 45.1, 32 of 2048 x 7168 (1792) 146 and 143.
+    if (CG == 1 && (MODE == kLinear || MODE == kRowsGrad) && (int64_t)p.seg.E * ((p.F + 127) / 128) <= dev.sms) p.span = 128;
     p.stage_bytes = (p.span == 128 && !gated(MODE) ? 1 : kHalves) * kHalfBytes + p.most / CG * 128;
     p.accs = 2 * kHalves * p.most <= kColumns ? 2 : 1;
     // a tile of results per column group, and one for each array of saved products (the gated block in pairs has room for two in turn)

@@ -26,6 +26,7 @@ SINGLE = [0 if i % 6 == 5 else 100 if i == 22 else (i * 7) % 41 for i in range(4
 SEGMENTS = {
     "pairs": (2, 2500, _in_regions(PAIRS, 2, 3)),      # 138 rows of capacity per expert, and more than 32 experts
     "single": (2, 600, _in_regions(SINGLE, 2, 1)),     # 30
+    "narrow": (2, 570, _in_regions([0 if i == 7 else 90 if i % 2 else 10 for i in range(18)], 2, 0)),   # 63
 }
 
 
@@ -52,8 +53,7 @@ def tiles(name, features, span):
 
 def wide(name, features):
     """Features per tile of a product with one matrix per expert."""
-    E = len(SEGMENTS[name][2])
-    return 256 if name == "pairs" or E * -(-features // 256) >= 4 * units(name) else 128
+    return 256 if name == "pairs" or len(SEGMENTS[name][2]) * -(-features // 128) > units(name) else 128
 
 
 @pytest.mark.parametrize("name,H,I", [("pairs", 136, 1032), ("single", 136, 2056)])
@@ -68,14 +68,14 @@ def test_gated_takes_fp8_rows(many, name, H, I):
     X.test_gated_takes_fp8_rows(name, H, I)
 
 
-@pytest.mark.parametrize("name,K,N,span", [("pairs", 136, 2056, 256), ("single", 136, 2056, 128), ("single", 72, 3848, 256)])
+@pytest.mark.parametrize("name,K,N,span", [("pairs", 136, 2056, 256), ("single", 136, 3848, 256), ("narrow", 72, 1016, 128)])
 def test_linear(many, name, K, N, span):
-    assert wide(name, N) == span and tiles(name, N, span) >= 3 * units(name)
+    assert wide(name, N) == span and tiles(name, N, span) >= (1.3 if name == "narrow" else 3) * units(name)
     X.test_linear(name, K, N)
 
 
 # (the rows' gradient has the width of the rows as its features; the weights' gradient tiles of 256 x 256 of every expert)
-@pytest.mark.parametrize("name,H,I", [("pairs", 2056, 72), ("pairs", 72, 1032), ("single", 2056, 72), ("single", 72, 2056), ("single", 3848, 40)])
+@pytest.mark.parametrize("name,H,I", [("pairs", 2056, 72), ("pairs", 72, 1032), ("single", 72, 2056), ("single", 3848, 72)])
 def test_gated_backward(many, name, H, I):
     E = len(SEGMENTS[name][2])
     assert E * -(-H // 256) * -(-2 * I // 256) >= 3 * units(name) or tiles(name, H, wide(name, H)) >= 3 * units(name)
@@ -87,13 +87,20 @@ def test_gated_backward_takes_fp8_rows(many, name, H, I):
     X.test_gated_backward_takes_fp8_rows(name, H, I)
 
 
-@pytest.mark.parametrize("name,K,N,span", [("pairs", 2056, 136, 256), ("pairs", 136, 2056, 256), ("single", 2056, 264, 128),
-                                           ("single", 3848, 72, 256), ("single", 72, 3848, 128)])
+@pytest.mark.parametrize("name,K,N,span", [("pairs", 2056, 136, 256), ("pairs", 136, 2056, 256), ("single", 3848, 72, 256),
+                                           ("single", 72, 3848, 128)])
 def test_linear_backward(many, name, K, N, span):
     E = len(SEGMENTS[name][2])
     assert wide(name, K) == span
     assert E * -(-K // 256) * -(-N // 256) >= 3 * units(name) and (K < N or tiles(name, K, span) >= 3 * units(name))
     X.test_linear_backward(name, K, N)
+
+
+# (narrow tiles are taken where there is an SM for each: a second one comes from experts with more than 64 rows)
+@pytest.mark.parametrize("K,N", [(1016, 72), (72, 1016)])
+def test_linear_backward_in_narrow_tiles(many, K, N):
+    assert wide("narrow", K) == 128 and (K < N or tiles("narrow", K, 128) >= 1.3 * units("narrow"))
+    X.test_linear_backward("narrow", K, N)
 
 
 # columns of a thread: 8 up to N = 2048, then 16, 32 and 64; without a row weight's gradient more than 8192 columns are split
