@@ -410,11 +410,12 @@ def ubep_expert_segments(buf) -> ubep_expert_rows_t:
 # ------------------------------------------------------------------ router and experts
 #
 # Sizes are taken from the tensors; a tensor of another type, shape or device raises ValueError.  Outputs left at None
-# are allocated (rows of no segment are not written).  The arithmetic is described in include/ubep.h.
+# are allocated (rows of no segment are not written), from the pool of the stream that the call runs on.  The calls keep no
+# history for autograd: the ``..._backward`` calls are made by hand.  The arithmetic is described in include/ubep.h.
 
 class ExpertRows:
     """Which rows of arrays [ranks, rows, width] belong to which expert: ``offset`` and ``count``, int32 [experts] on the
-    GPU, relative to the expert's rank's region; ``status``, int32 [1], gets UBEP_ERR_TIMEOUT (None: nobody is told)."""
+    GPU, relative to the expert's rank's region; ``status``, int32 [1], gets UBEP_ERR_TIMEOUT (None: nobody is told of a wait that ran out)."""
     __slots__ = ("offset", "count", "status")
 
     def __init__(self, offset: torch.Tensor, count: torch.Tensor, status: Optional[torch.Tensor] = None):
